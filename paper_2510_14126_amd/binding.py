@@ -2,7 +2,8 @@
 the functions a serving loop calls every step the native ``_pycall`` extension.
 
 Every function here has the name and argument order of the C function it
-calls; see ``include/paged_attn.h`` for meanings, layouts and ownership.
+calls; see ``include/paged_attn.h`` and ``include/paged_attn_ops.h`` for
+meanings, layouts and ownership.
 Device buffers may be given as torch tensors (their ``data_ptr()`` is
 passed) or as raw integer addresses; ``stream`` is a HIP stream handle as an
 integer (for example ``torch.cuda.current_stream().cuda_stream``) or None
@@ -23,7 +24,12 @@ LIB_PATH = os.path.join(HERE, "libpaged_attn.so")
 PA_OK, PA_EINVAL, PA_ENOMEM, PA_EUNSUPPORTED, PA_EHIP, PA_ESTATE = 0, -1, -2, -3, -4, -5
 BLOCK_SIZE = 16
 
-# Every symbol the header declares, with (restype, argtypes).
+# Element types of rows, layouts of a rotated row, scalings of its frequencies.
+PA_BF16, PA_FP16, PA_FP32 = 0, 1, 2
+PA_ROPE_HALF, PA_ROPE_INTERLEAVED = 0, 1
+PA_ROPE_UNSCALED, PA_ROPE_LINEAR, PA_ROPE_NTK, PA_ROPE_BANDS, PA_ROPE_YARN = 0, 1, 2, 3, 4
+
+# Every symbol that paged_attn.h declares, with (restype, argtypes).
 _c_int, _i32, _i64, _f32, _vp, _sz = (ctypes.c_int, ctypes.c_int32, ctypes.c_int64,
                                       ctypes.c_float, ctypes.c_void_p, ctypes.c_size_t)
 _pi32 = ctypes.POINTER(ctypes.c_int32)
@@ -92,6 +98,24 @@ SIGNATURES = {
                                            _i32, _vp, _vp]),
 }
 
+# The same for paged_attn_ops.h.
+_f64 = ctypes.c_double
+_pf64 = ctypes.POINTER(ctypes.c_double)
+OPS_SIGNATURES = {
+    "pa_rope_frequencies": (_c_int, [_i32, _f64, _i32, _f64, _f64, _f64, _f64, _pf64, _pf64]),
+    "pa_rope_create": (_c_int, [_i32, _i32, _i32, _pf64, _f64, ctypes.POINTER(_vp)]),
+    "pa_rope_destroy": (_c_int, [_vp]),
+    "paged_attn_norm_rope": (_c_int, [_vp, _vp, _i64, _i32, _vp, _vp, _i64, _i32, _vp, _f32, _i32, _vp, _i32, _vp,
+                                      _i64, _vp, _i64, _vp]),
+    "paged_attn_rope_append": (_c_int, [_vp, _vp, _vp, _i64, _i32, _vp, _vp, _i64, _vp, _vp, _i64, _f32, _i32, _vp,
+                                        _vp, _i32, _vp, _i32, _vp, _i32, _vp, _vp]),
+    "paged_attn_biased_workspace_size": (_c_int, [_vp, _i32, _i32, _i32, _i32, _i32, ctypes.POINTER(_sz)]),
+    "paged_attn_decode_biased": (_c_int, [_vp, _vp, _vp, _i32, _vp, _i32, _i32, _f32, _f32, _vp, _i32, _vp, _i32,
+                                          _vp, _sz, _vp, _vp]),
+    "paged_attn_extend_biased": (_c_int, [_vp, _vp, _vp, _i32, _vp, _i32, _vp, _i32, _i32, _f32, _f32, _vp, _i32,
+                                          _vp, _vp, _i32, _i32, _vp, _sz, _vp, _vp]),
+}
+
 
 class PagedAttnError(RuntimeError):
     def __init__(self, code: int, message: str):
@@ -110,7 +134,7 @@ def _load(path: str = LIB_PATH) -> ctypes.CDLL:
             f"{path} is missing: build the HIP library first "
             "(python -c 'import __graft_entry__ as g; g.build()')")
     lib = ctypes.CDLL(path)
-    for name, (res, args) in SIGNATURES.items():
+    for name, (res, args) in {**SIGNATURES, **OPS_SIGNATURES}.items():
         fn = getattr(lib, name)
         fn.restype = res
         fn.argtypes = args
@@ -122,7 +146,8 @@ def _load(path: str = LIB_PATH) -> ctypes.CDLL:
 PER_STEP = ("paged_attn_decode", "paged_attn_decode_scheduled", "paged_attn_reduce", "paged_attn_decode_cascade",
             "paged_attn_decode_cascade_scheduled", "paged_attn_decode_cascade_groups", "paged_attn_reduce_cascade",
             "paged_attn_reduce_cascade_groups", "paged_attn_append_kv", "paged_attn_decode_append",
-            "paged_attn_decode_cascade_append", "paged_attn_decode_noalloc", "paged_attn_extend")
+            "paged_attn_decode_cascade_append", "paged_attn_decode_noalloc", "paged_attn_extend",
+            "paged_attn_norm_rope", "paged_attn_rope_append", "paged_attn_decode_biased", "paged_attn_extend_biased")
 
 
 def _ctypes_call(lib: ctypes.CDLL, name: str):
@@ -513,3 +538,98 @@ def paged_attn_decode_noalloc(pool: KVPool, q, block_tables, bt_stride, context_
     _check(_pycall.paged_attn_decode_noalloc(pool._handle(), q, block_tables, bt_stride,
                                              context_lens, batch, num_q_heads, scale,
                                              max_context_len, partition_size, out, stream))
+
+
+class Rope:
+    """Handle of a rotation (host metadata)."""
+
+    def __init__(self, handle: int, head_dim: int, rotary_dim: int, layout: int):
+        self.handle = handle
+        self.head_dim = head_dim
+        self.rotary_dim = rotary_dim
+        self.layout = layout
+
+    def close(self) -> None:
+        if self.handle:
+            _lib.pa_rope_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def __enter__(self):
+        return self
+
+    def __exit__(self, *exc):
+        self.close()
+
+    def _handle(self):
+        if not self.handle:
+            raise PagedAttnError(PA_EINVAL, "rope handle is closed")
+        return self.handle
+
+
+def pa_rope_frequencies(rotary_dim, base, scaling=PA_ROPE_UNSCALED, factor=1.0, original_context=0.0, low=0.0,
+                        high=0.0):
+    """Returns (frequencies, a list of rotary_dim / 2 floats; magnitude)."""
+    freqs = (ctypes.c_double * max(1, rotary_dim // 2))()
+    magnitude = ctypes.c_double()
+    _check(_lib.pa_rope_frequencies(rotary_dim, base, scaling, factor, original_context, low, high, freqs,
+                                    ctypes.byref(magnitude)))
+    return list(freqs)[: rotary_dim // 2], magnitude.value
+
+
+def pa_rope_create(head_dim, rotary_dim, layout, freqs, magnitude=1.0) -> Rope:
+    freqs = [float(f) for f in freqs]
+    if len(freqs) < rotary_dim // 2:
+        raise PagedAttnError(PA_EINVAL, f"pa_rope_create: {len(freqs)} frequencies for rotary_dim = {rotary_dim}")
+    arr = (ctypes.c_double * max(1, len(freqs)))(*freqs)
+    h = ctypes.c_void_p()
+    _check(_lib.pa_rope_create(head_dim, rotary_dim, layout, arr, magnitude, ctypes.byref(h)))
+    return Rope(h.value, head_dim, rotary_dim, layout)
+
+
+def pa_rope_destroy(rope: Rope) -> None:
+    rope.close()
+
+
+def paged_attn_norm_rope(rope: Rope, q, q_stride, num_q_heads, q_weight, k, k_stride, num_kv_heads, k_weight, eps,
+                         dtype, positions, tokens, q_out, q_out_stride, k_out, k_out_stride, stream=None) -> None:
+    _check(_pycall.paged_attn_norm_rope(rope._handle(), q, q_stride, num_q_heads, q_weight, k, k_stride,
+                                        num_kv_heads, k_weight, eps, dtype, positions, tokens, q_out, q_out_stride,
+                                        k_out, k_out_stride, stream))
+
+
+def paged_attn_rope_append(pool: KVPool, rope: Rope, q, q_stride, num_q_heads, q_weight, k, k_stride, k_weight, v,
+                           v_stride, eps, dtype, positions, q_start, total_q, block_tables, bt_stride, context_lens,
+                           batch, q_out, stream=None) -> None:
+    _check(_pycall.paged_attn_rope_append(pool._handle(), rope._handle(), q, q_stride, num_q_heads, q_weight, k,
+                                          k_stride, k_weight, v, v_stride, eps, dtype, positions, q_start, total_q,
+                                          block_tables, bt_stride, context_lens, batch, q_out, stream))
+
+
+def paged_attn_biased_workspace_size(pool: KVPool, batch, num_q_heads, max_context_len, max_chunk=1, window=0) -> int:
+    n = ctypes.c_size_t()
+    _check(_lib.paged_attn_biased_workspace_size(pool._handle(), batch, num_q_heads, max_context_len, max_chunk,
+                                                 window, ctypes.byref(n)))
+    return n.value
+
+
+def paged_attn_decode_biased(pool: KVPool, q, block_tables, bt_stride, context_lens, batch, num_q_heads, scale,
+                             softcap, slopes, window, first_tokens, max_context_len, workspace, workspace_bytes, out,
+                             stream=None) -> None:
+    _check(_pycall.paged_attn_decode_biased(pool._handle(), q, block_tables, bt_stride, context_lens, batch,
+                                            num_q_heads, scale, softcap, slopes, window, first_tokens,
+                                            max_context_len, workspace, workspace_bytes, out, stream))
+
+
+def paged_attn_extend_biased(pool: KVPool, q, q_start, total_q, block_tables, bt_stride, context_lens, batch,
+                             num_q_heads, scale, softcap, slopes, window, first_tokens, prefix_lens, max_context_len,
+                             max_chunk, workspace, workspace_bytes, out, stream=None) -> None:
+    _check(_pycall.paged_attn_extend_biased(pool._handle(), q, q_start, total_q, block_tables, bt_stride,
+                                            context_lens, batch, num_q_heads, scale, softcap, slopes, window,
+                                            first_tokens, prefix_lens, max_context_len, max_chunk, workspace,
+                                            workspace_bytes, out, stream))

@@ -20,7 +20,8 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD_DIR = os.path.join(HERE, "_build")
 LIB_PATH = os.path.join(HERE, "libpaged_attn.so")
 SOURCES = ["api.cpp", "decode_mfma.hip", "cascade.hip", "reduce.hip", "append.hip", "extend.hip",
-           "stream_copy.hip", "gather_tiles.hip", "noalloc.hip"]
+           "stream_copy.hip", "gather_tiles.hip", "noalloc.hip", "api_ops.cpp", "rope.hip",
+           "biased.hip"]
 PYCALL_PATH = os.path.join(HERE, "_pycall" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
 ARCH = "gfx950"
 

@@ -3,6 +3,7 @@
 // before any HIP call, so all validation paths work without a GPU.
 #include "paged_attn.h"
 #include "kernels.h"
+#include "pool.h"
 
 #include <hip/hip_runtime.h>
 
@@ -11,18 +12,6 @@
 #include <cstdio>
 #include <string>
 #include <vector>
-
-struct pa_kv_pool {
-  int32_t num_blocks;
-  int32_t num_kv_heads;
-  int32_t head_dim;
-  uint16_t* k;                     // caller-owned device pools (the append writes them)
-  uint16_t* v;
-  std::vector<int32_t> refcount;  // 0 = free
-  std::vector<int32_t> free_stack; // top = back(); ids pop in ascending order initially
-  int64_t shared_blocks = 0;       // blocks whose reference count is 2 or more
-  int64_t shared_refs = 0;         // references of those blocks
-};
 
 namespace {
 thread_local std::string g_err = "no error";

@@ -1,0 +1,618 @@
+// Attention of query rows over a paged context with capped, biased or masked
+// scores, on 32x32 MFMA tiles (gfx950, head_dim 64 or 128).
+//
+// For KV head g the (new token i, head j) pairs of sequence b form rows
+// R = i * G + j, at position p = n - L + i (n: context with the L new tokens).
+// In log2 units, x = |scale| log2(e) <q, K[t]> (a negative scale rides on the
+// sign of Q),
+//     y = cap tanh(x / cap)      (CAP)        y = x            (else)
+//     e = y - slope |p - t|      (BIAS)
+// for the tokens lo <= t < hi that the row sees, and out = sum 2^e V / sum 2^e.
+//
+// tanh: tanh(z) / z is even, so while |z| <= 1/2 a polynomial of degree three in
+// raw^2 (minimax, relative error 5.5e-7) gives y in four FMAs and one product,
+// without the transcendental unit that the softmax keeps busy; a stage with any
+// larger score (rare: caps are chosen well above ordinary scores) takes cap -
+// 2 cap / (2^(2 z log2 e) + 1) for those.
+//
+// Lanes: h = lane >> 5, n = lane & 31.  v_mfma_f32_32x32x16_bf16 takes A row n
+// / B column n at contraction indices 8h .. 8h+7 and leaves in register r of
+// its result row 8(r/4) + 4h + r%4 of column n.  A stage is 32 tokens, K rows
+// then V rows in LDS.
+//  * S^T = K Q^T: A = K rows (token i of the stage in row i), B = Q^T with query
+//    row n in column n.  Lane (h, n) receives the scores of tokens 8a + 4h + b
+//    (register 4a + b).
+//  * O += P V: for block m of the stage the contraction index k = 8h + e
+//    stands for token 16m + 8(e/4) + 4h + e%4, which makes the scores above
+//    exactly the A operand; the B operand comes from the staged V through
+//    transposing reads.  Each weight reaches the matrix core as a bf16 pair,
+//    high part and rounded remainder (about 2^-17 relative); the row sum adds
+//    the fp32 values.
+//
+// What hidden tokens hold must not matter.  Tokens that no row of the workgroup
+// sees are staged as zeros.  Where some rows see a token and others do not its
+// weight is an exact 0, but 0 times an infinity or NaN in V is NaN in an MFMA:
+// in stages with masks, infinities and NaN of V are staged as zeros too, and a
+// second pass over those stages (add_special, only where there were any) adds
+// them to the rows that do see them.
+#pragma once
+
+#include "kernels.h"
+#include "mfma_body.h"
+#include "ops.h"
+#include "pa_device.h"
+
+namespace pa {
+namespace biased {
+
+using mfma::bf16x8_t;
+using mfma::floatx16_t;
+using mfma::floatx4_t;
+using mfma::kLazyRescale;
+using mfma::kWaves;
+using mfma::lds_floatx4_t;
+using mfma::lds_short4_t;
+using mfma::lds_u32x4_t;
+using mfma::pack_bf16;
+using mfma::u32x4_t;
+typedef __attribute__((address_space(3))) uint16_t lds_u16_t;
+
+constexpr int kTokens = 32;                                 // per stage: two blocks
+template <int D> constexpr int kStageBytes = 2 * kTokens * D * 2;   // K rows, then V rows
+template <int D> constexpr int kVOffset = kTokens * D * 2;
+template <int D> constexpr int kPieces = D / 32;            // 16-byte pieces of K (and of V) per lane and 16 tokens, x 2
+
+// LDS byte offset of 16-byte chunk c of token row r of the staged K: chunk c at
+// position c ^ r modulo the row's chunks.  Lanes read one chunk column of 32
+// rows: eight consecutive ones touch eight different positions.
+template <int D>
+__device__ __forceinline__ int k_off(int r, int c) {
+  return r * (2 * D) + ((c ^ (r & (D / 8 - 1))) << 4);
+}
+
+// The same of the staged V (from kVOffset): 32-byte windows of 16 dims.  The
+// transposing reads of a half wavefront take windows 2j and 2j+1 of four
+// consecutive rows; at D = 128 a row spans all 64 banks and window w is at
+// w ^ 2(r % 4), at D = 64 two rows do and it is at w ^ 2(r / 2 % 2).
+template <int D>
+__device__ __forceinline__ int v_off(int r, int c) {
+  const int swz = D == 128 ? (r & 3) << 1 : (r & 2);
+  return r * (2 * D) + (((c >> 1) ^ swz) << 5) + ((c & 1) << 4);
+}
+
+// Maximum over the 32 columns; every lane receives it (both halves hold the
+// same columns).
+template <int CTRL>
+__device__ __forceinline__ int dpp_i(int x) { return __builtin_amdgcn_mov_dpp(x, CTRL, 0xf, 0xf, true); }
+__device__ __forceinline__ int max32(int x) {
+  x = max(x, dpp_i<kDppQuadXor1>(x));
+  x = max(x, dpp_i<kDppQuadXor2>(x));
+  x = max(x, dpp_i<kDppRowRor4>(x));
+  x = max(x, dpp_i<kDppRowRor8>(x));
+  const auto y = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  return wave_uniform(max((int)y[0], (int)y[1]));
+}
+__device__ __forceinline__ int min32(int x) { return -max32(-x); }
+
+// Sequence b's new tokens: its first row in q and out, their number, the
+// position of the first and the context length.  Device data, clamped.
+struct Chunk {
+  int start, len, first, ctx;
+};
+__device__ __forceinline__ Chunk chunk_of(const BiasedParams& p, int b) {
+  int ctx = p.context_lens[b];
+  ctx = ctx < 0 ? 0 : (ctx > p.max_ctx ? p.max_ctx : ctx);
+  int qs = b, L = 1;
+  if (p.q_start) {
+    qs = p.q_start[b];
+    qs = qs < 0 ? 0 : (qs > p.total_q ? p.total_q : qs);
+    const int qe = p.q_start[b + 1];
+    L = qe < qs ? 0 : (qe > p.total_q ? p.total_q : qe) - qs;
+  }
+  L = min(min(L, ctx), p.max_chunk);
+  return {qs, L, ctx - L, ctx};
+}
+
+// What the row of column n sees, and its bias.
+struct Row {
+  int lo, hi;       // tokens lo <= t < hi; hi <= lo: none
+  float pos;
+  float slope;      // log2 units per token of distance
+};
+template <bool BIAS>
+__device__ __forceinline__ Row row_of(const BiasedParams& p, const Chunk& c, int b, int g, int R) {
+  const int i = R / p.group;
+  const int pos = c.first + i;
+  Row r;
+  r.lo = p.window > 0 ? max(0, pos - p.window + 1) : 0;
+  if (p.first_tokens) r.lo = max(r.lo, min(p.first_tokens[c.start + i], c.ctx));
+  r.hi = pos + 1;
+  if (p.prefix_lens) r.hi = max(r.hi, min(p.prefix_lens[b], c.ctx));
+  r.hi = max(r.hi, r.lo);
+  r.pos = (float)pos;
+  r.slope = BIAS ? p.slopes[g * p.group + R % p.group] * kLog2e : 0.f;
+  return r;
+}
+
+// The 32 columns of one wavefront: queries (Q^T operand of step s: dims 16s + 8h
+// .. of column n), softmax state, outputs.
+template <int D, bool CAP, bool BIAS>
+struct Columns {
+  Row row;
+  float m, neg, l;              // running max, -m (0 while it is -inf), the lane's share of the sum
+  floatx16_t o[D / 32];         // [j][r]: row 8(r/4) + 4h + r%4, dim 32j + n
+  float scale;                  // |scale_log2|
+
+  // Operand of step s from the row's memory; bf16 negation is exact.
+  static __device__ __forceinline__ u32x4_t query(const BiasedParams& p, const uint16_t* q_row, int s, int h) {
+    const uint32_t flip = p.scale_log2 < 0.f ? 0x80008000u : 0u;
+    const uint4 w = *reinterpret_cast<const uint4*>(q_row + (2 * s + h) * 8);
+    return u32x4_t{w.x ^ flip, w.y ^ flip, w.z ^ flip, w.w ^ flip};
+  }
+
+  __device__ __forceinline__ void init(const BiasedParams& p, const Row& r) {
+    // A scale of zero becomes the smallest normal number, so that a hidden
+    // token's score stays -inf times it (ordinary scores weigh the same).
+    scale = p.scale_log2 == 0.f ? 1.1754944e-38f : fabsf(p.scale_log2);
+    row = r;
+    m = -__builtin_inff();
+    neg = 0.f;
+    l = 0.f;
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) o[j][i] = 0.f;
+  }
+
+  // Raw scores of the stage at st; q(s): the operand of step s.
+  template <typename Q>
+  static __device__ __forceinline__ floatx16_t scores(const lds_u8_t* st, int h, int n, Q&& q) {
+    floatx16_t a;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) a[i] = 0.f;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s)
+      a = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+          __builtin_bit_cast(bf16x8_t, *reinterpret_cast<const lds_u32x4_t*>(st + k_off<D>(n, 2 * s + h))),
+          __builtin_bit_cast(bf16x8_t, q(s)), a, 0, 0, 0);
+    return a;
+  }
+
+  // Cap, bias and masks of a stage whose first token is t0.  With CAP or BIAS
+  // the scores become log2 units; else they stay raw.
+  __device__ __forceinline__ void shape(const BiasedParams& p, floatx16_t& a, int t0, bool edge, int h) const {
+    if constexpr (CAP) {
+      float most = 0.f;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) most = fmaxf(most, fabsf(a[r]));
+      const bool far = __builtin_amdgcn_ballot_w64(!(most <= p.raw_max)) != 0;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float x = a[r], u = x * x;
+        float y = x * fmaf(u, fmaf(u, fmaf(u, p.c3, p.c2), p.c1), p.c0);
+        if (far) {
+          const float t = fast_exp2(x * p.two_z);
+          const float z = fmaf(-2.f * p.cap, __builtin_amdgcn_rcpf(t + 1.f), p.cap);
+          y = fabsf(x) <= p.raw_max ? y : z;
+        }
+        a[r] = y;
+      }
+    }
+    if constexpr (BIAS) {
+      const float d0 = row.pos - (float)(t0 + 4 * h);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float y = CAP ? a[r] : a[r] * scale;
+        a[r] = fmaf(-row.slope, fabsf(d0 - (float)(8 * (r >> 2) + (r & 3))), y);
+      }
+    }
+    if (edge) {
+      const int from = t0 + 4 * h - row.lo;
+      const unsigned span = (unsigned)(row.hi - row.lo);
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if ((unsigned)(from + 8 * (r >> 2) + (r & 3)) >= span) a[r] = -__builtin_inff();
+    }
+  }
+
+  __device__ __forceinline__ float weight(float a) const {
+    return fast_exp2(CAP || BIAS ? a + neg : fmaf(a, scale, neg));
+  }
+
+  // One value per row, from the lane (h, n) that holds it as column n to the
+  // lanes that hold the row's outputs.  rowv: 32 floats of the wavefront's own.
+  static __device__ __forceinline__ void per_row(lds_f32_t* rowv, int h, int n, float x, float (&out)[16]) {
+    if (h == 0) rowv[n] = x;
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int a = 0; a < 4; ++a) {
+      const floatx4_t y = *reinterpret_cast<const lds_floatx4_t*>(rowv + 8 * a + 4 * h);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) out[4 * a + e] = y[e];
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+
+  // Running-max step before a stage's weights.  The test needs no cross-lane
+  // reduction: any lane above its row's max + kLazyRescale triggers the rescale.
+  __device__ __forceinline__ void raise(const floatx16_t& a, lds_f32_t* rowv, int h, int n) {
+    float x = a[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) x = fmaxf(x, a[r]);
+    if (!(CAP || BIAS)) x *= scale;
+    if (__builtin_amdgcn_ballot_w64(x > m + kLazyRescale) != 0) {
+      float y = x;
+      swap32(x, y);
+      const float bm = fmaxf(x, y);
+      const float mn = bm > m + kLazyRescale ? bm : m;
+      // 1 for rows that keep their max (or have attended to nothing yet)
+      const float alpha = mn == -__builtin_inff() ? 1.f : fast_exp2(m - mn);
+      l *= alpha;
+      if (__builtin_amdgcn_ballot_w64(m != -__builtin_inff()) != 0) {
+        float ar[16];
+        per_row(rowv, h, n, alpha, ar);
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[j][r] *= ar[r];
+      }
+      m = mn;
+      neg = mn == -__builtin_inff() ? 0.f : -mn;
+    }
+  }
+
+  // Weights of the shaped scores a and their PV with the stage at st.
+  __device__ __forceinline__ void attend(const floatx16_t& a, const lds_u8_t* st, int lane) {
+    u32x4_t hi[2], lo[2];
+    float sum[2];
+#pragma unroll
+    for (int mb = 0; mb < 2; ++mb)
+#pragma unroll
+      for (int e = 0; e < 8; e += 2) {
+        const float p0 = weight(a[8 * mb + e]), p1 = weight(a[8 * mb + e + 1]);
+        const uint32_t w = pack_bf16(p0, p1);
+        hi[mb][e / 2] = w;
+        lo[mb][e / 2] = pack_bf16(p0 - bf16_lo(w), p1 - bf16_hi(w));
+        sum[mb] = e == 0 ? p0 + p1 : sum[mb] + (p0 + p1);
+      }
+    l += sum[0] + sum[1];
+    // Transposing reads: lane i = lane % 16 of group (h, f = bit 4 of lane)
+    // addresses row 4h + i/4 (+ 8u, + 16m), dims 32j + 16f + 4(i%4) .. +3.
+    const int vr = 4 * (lane >> 5) + ((lane & 15) >> 2);
+    const int vf = (lane >> 4) & 1;
+#pragma unroll
+    for (int mb = 0; mb < 2; ++mb) {
+      u32x4_t vb[D / 32];
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) {
+        uint2 b[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          b[u] = __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                     (lds_short4_t*)(st + kVOffset<D> + mb * 16 * D * 2 + v_off<D>(vr + 8 * u, 2 * (2 * j + vf)) +
+                                     ((lane & 3) << 3))));
+        vb[j] = u32x4_t{b[0].x, b[0].y, b[1].x, b[1].y};
+      }
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j)
+        o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, hi[mb]),
+                                                       __builtin_bit_cast(bf16x8_t, vb[j]), o[j], 0, 0, 0);
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j)
+        o[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, lo[mb]),
+                                                       __builtin_bit_cast(bf16x8_t, vb[j]), o[j], 0, 0, 0);
+    }
+  }
+
+  // Adds what stood in V where a masked stage was given zeros for infinities and
+  // NaN, to the rows that see it (its weight is above 0: it makes them infinite
+  // or NaN).  st: the stage's V as it is, first token t0.  rowv: 32 floats of LDS
+  // of the wavefront's own.
+  __device__ __forceinline__ void add_special(int t0, const lds_u8_t* st, lds_f32_t* rowv, int h, int n) {
+    float from[16], to[16];
+    per_row(rowv, h, n, __int_as_float(row.lo), from);
+    per_row(rowv, h, n, __int_as_float(row.hi), to);
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j) {
+#pragma unroll 1
+      for (int t = 0; t < kTokens; ++t) {
+        const uint32_t x = *reinterpret_cast<const lds_u16_t*>(st + kVOffset<D> + v_off<D>(t, (32 * j + n) >> 3) +
+                                                               ((n & 7) << 1));
+        const float v = (x & 0x7f80u) == 0x7f80u ? bf16_lo(x) : 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (t0 + t >= __float_as_int(from[r]) && t0 + t < __float_as_int(to[r])) o[j][r] += v;
+      }
+    }
+  }
+};
+
+// A packed pair of bf16 with zeros for infinities and NaN; marks them in `odd`.
+__device__ __forceinline__ uint32_t finite_part(uint32_t x, uint32_t& odd) {
+  const uint32_t bad = (((x & 0x7f807f80u) + 0x00800080u) >> 15) & 0x00010001u;   // an exponent of all ones carries
+  odd |= bad;
+  return x & ~(bad * 0xffffu);
+}
+
+// --------------------------------------------------------------------------
+// One row tile per workgroup, its tokens split over the wavefronts (and over
+// workgroups, `parts`): for decode, short chunks and small grids.
+// --------------------------------------------------------------------------
+template <int D> constexpr int kSwapBytes = 4 * 64 * (D / 32) * 4;     // one wavefront's outputs for another at the merge
+template <int D> constexpr int kSplitStats = kWaves * kStageBytes<D>;
+template <int D> constexpr int kSplitQuery = kSplitStats<D> + 3 * kWaves * kBiasedTileRows * 4;   // the tile's queries
+template <int D> constexpr int kSplitLdsBytes = kSplitQuery<D> + kBiasedTileRows * D * 2;
+static_assert(kWaves * (kWaves - 1) * kSwapBytes<128> <= kSplitStats<128>, "the merge reuses the stages");
+static_assert(kWaves * (kWaves - 1) * kSwapBytes<64> <= kSplitStats<64>, "the merge reuses the stages");
+
+template <int D, bool CAP, bool BIAS>
+__device__ __forceinline__ void split_body(const BiasedParams& p, int wg, lds_u8_t* smem) {
+  constexpr int kRows = kBiasedTileRows;
+  const int lane = threadIdx.x & 63;
+  const int wave = wave_uniform(threadIdx.x >> 6);
+  const int h = lane >> 5;
+  const int n = lane & 31;
+
+  const int g = wg % p.num_kv_heads;
+  wg /= p.num_kv_heads;
+  const int tile = wg % p.tiles;
+  wg /= p.tiles;
+  const int b = wg % p.batch;
+  const int part = wg / p.batch;
+
+  const Chunk c = chunk_of(p, b);
+  const int rows = c.len * p.group;
+  const int row0 = tile * kRows;
+  if (row0 >= rows && !(p.q_start == nullptr && c.len == 0 && part == 0)) return;   // whole workgroup: no rows here
+  if (c.len == 0) {
+    // an empty sequence of a decode: its rows are zeros
+    for (int i = threadIdx.x; i < min(kRows, p.group - row0) * D; i += 64 * kWaves)
+      p.out[((size_t)b * p.num_q_heads + g * p.group + row0 + i / D) * D + i % D] = 0;
+    return;
+  }
+
+  // A column without a row repeats the tile's first and is not written.
+  const int R = row0 + n < rows ? row0 + n : row0;
+  const Row row = row_of<BIAS>(p, c, b, g, R);
+  const bool none = row.hi <= row.lo;
+  const int lo = min32(none ? 0x3fffffff : row.lo);     // tokens that some row sees
+  const int hi = max32(none ? 0 : row.hi);
+  const int all_lo = max32(row.lo);                     // tokens that every row sees
+  const int all_hi = min32(none ? 0 : row.hi);
+
+  // This partition's blocks.
+  const int first = lo >> 4;
+  const int nblk = hi > lo ? ((hi + 15) >> 4) - first : 0;
+  const int per = p.parts == 1 ? nblk : max(p.min_blocks, ((nblk + p.parts - 1) / p.parts + 1) & ~1);
+  const int j0 = first + part * per;
+  const int cnt = min(per, nblk - part * per);          // <= 0: nothing in this partition
+  const size_t slot = (((size_t)b * p.tiles + tile) * p.num_kv_heads + g) * p.parts + part;
+  if (cnt <= 0 && p.parts > 1) {
+    if (threadIdx.x < p.tile_rows) p.part_lse[slot * p.tile_rows + threadIdx.x] = -__builtin_inff();
+    return;
+  }
+
+  Columns<D, CAP, BIAS> C;
+  C.init(p, row);
+  // The queries stay in LDS (all wavefronts have the same rows): in registers
+  // they would not fit beside a stage in flight.
+  lds_u32x4_t* ql = reinterpret_cast<lds_u32x4_t*>(smem + kSplitQuery<D>) + lane;
+  {
+    const uint16_t* q_row = p.q + ((size_t)(c.start + R / p.group) * p.num_q_heads + g * p.group + R % p.group) * D;
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) {
+      const int s = wave * (D / 64) + i;
+      ql[64 * s] = C.query(p, q_row, s, h);
+    }
+  }
+
+  constexpr size_t kTile = 16 * D;
+  const size_t blk_stride = (size_t)p.num_kv_heads * kTile;
+  const uint16_t* kbase = p.k_pool + (size_t)g * kTile;
+  const uint16_t* vbase = p.v_pool + (size_t)g * kTile;
+  const int32_t* bt = p.block_tables + (size_t)b * p.bt_stride + j0;
+
+  // A wavefront's stage: kLoads pieces of K and of V per lane, piece i of token
+  // row i * kRowsPerLoad + lane / (D/8).
+  constexpr int kChunks = D / 8;
+  constexpr int kRowsPerLoad = 64 / kChunks;
+  constexpr int kLoads = kTokens / kRowsPerLoad;
+  const int lrow = lane / kChunks, lchunk = lane % kChunks;
+  const int lane_off = lane * 16;
+  u32x4_t rk[kLoads], rv[kLoads];
+  const int nstage = (cnt + 1) >> 1;
+  // Block ids, one per lane: those of the 64 blocks being loaded and the next 64.
+  auto ids_of = [&](int chunk) {
+    const int j = 64 * chunk + lane;
+    return j < cnt ? min(max(bt[j], 0), p.num_blocks - 1) : 0;
+  };
+  int ids = ids_of(0), ids_next = ids_of(1), chunk = 0;
+  auto load = [&](int s) {
+    if (2 * s >> 6 != chunk) {                            // uniform; a wavefront's stages skip no chunk
+      ids = ids_next;
+      ids_next = ids_of(++chunk + 1);
+    }
+    int id[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) id[e] = __builtin_amdgcn_readlane(ids, (2 * s + e) & 63);
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int bytes = 2 * s + e < cnt ? (int)kTile * 2 : 0;      // none past the last block: zeros
+      const __amdgpu_buffer_rsrc_t dk = __builtin_amdgcn_make_buffer_rsrc(
+          const_cast<uint16_t*>(kbase + (size_t)id[e] * blk_stride), 0, bytes, kBufferDescWord3);
+      const __amdgpu_buffer_rsrc_t dv = __builtin_amdgcn_make_buffer_rsrc(
+          const_cast<uint16_t*>(vbase + (size_t)id[e] * blk_stride), 0, bytes, kBufferDescWord3);
+#pragma unroll
+      for (int i = 0; i < kLoads / 2; ++i) {
+        rk[e * kLoads / 2 + i] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(dk, lane_off + i * 1024, 0, 0));
+        rv[e * kLoads / 2 + i] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(dv, lane_off + i * 1024, 0, 0));
+      }
+    }
+  };
+
+  lds_u8_t* st = smem + wave * kStageBytes<D>;
+  lds_f32_t* sm = reinterpret_cast<lds_f32_t*>(smem + kSplitStats<D>);   // [kWaves][32]
+  lds_f32_t* sl = sm + kWaves * kRows;                                   // [kWaves][32]
+  lds_f32_t* rowv = sl + kWaves * kRows + wave * kRows;
+
+  uint32_t odd = 0;                                               // infinities or NaN among V where there are masks
+  load(wave);
+  __syncthreads();
+  for (int s = wave; s < nstage; s += kWaves) {
+    const int t0 = (j0 + 2 * s) * 16;
+    const bool edge = t0 < all_lo || t0 + kTokens > all_hi;       // uniform
+    if (edge) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int t = t0 + i * kRowsPerLoad + lrow;
+        if (t < lo || t >= hi) {
+          rk[i] = u32x4_t{0, 0, 0, 0};
+          rv[i] = u32x4_t{0, 0, 0, 0};
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) rv[i][e] = finite_part(rv[i][e], odd);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int r = i * kRowsPerLoad + lrow;
+      *reinterpret_cast<lds_u32x4_t*>(st + k_off<D>(r, lchunk)) = rk[i];
+      *reinterpret_cast<lds_u32x4_t*>(st + kVOffset<D> + v_off<D>(r, lchunk)) = rv[i];
+    }
+    load(s + kWaves);
+    floatx16_t a = C.scores(st, h, n, [&](int i) { return ql[64 * i]; });
+    C.shape(p, a, t0, edge, h);
+    C.raise(a, rowv, h, n);
+    C.attend(a, st, lane);
+  }
+
+  if (__builtin_amdgcn_ballot_w64(odd != 0) != 0) {
+#pragma unroll 1
+    for (int s = wave; s < nstage; s += kWaves) {
+      const int t0 = (j0 + 2 * s) * 16;
+      if (t0 >= all_lo && t0 + kTokens <= all_hi) continue;
+#pragma unroll 1
+      for (int r = lrow; r < kTokens; r += kRowsPerLoad) {
+        const int j = 2 * s + (r >> 4);
+        uint4 x = make_uint4(0, 0, 0, 0);
+        if (j < cnt) {
+          const size_t id = (size_t)min(max(bt[j], 0), p.num_blocks - 1);
+          x = *reinterpret_cast<const uint4*>(vbase + id * blk_stride + (r & 15) * D + lchunk * 8);
+        }
+        *reinterpret_cast<lds_u32x4_t*>(st + kVOffset<D> + v_off<D>(r, lchunk)) = u32x4_t{x.x, x.y, x.z, x.w};
+      }
+      __builtin_amdgcn_wave_barrier();
+      C.add_special(t0, st, rowv, h, n);
+      __builtin_amdgcn_wave_barrier();
+    }
+  }
+
+  // Merge.  Row n's maximum and sum over the wavefronts, then each wavefront
+  // scales its outputs to the common maximum and the final sum; wavefront d
+  // adds up rows 8d + 4h + b (b = 0..3).
+  {
+    float x = C.l, y = C.l;
+    swap32(x, y);
+    if (h == 0) {
+      sm[wave * kRows + n] = C.m;
+      sl[wave * kRows + n] = x + y;
+    }
+  }
+  __syncthreads();
+  float mx = sm[n];
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) mx = fmaxf(mx, sm[w * kRows + n]);
+  const float mref = mx == -__builtin_inff() ? 0.f : mx;
+  float lt = 0.f;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) lt = fmaf(sl[w * kRows + n], fast_exp2(sm[w * kRows + n] - mref), lt);
+  const float inv = lt == 0.f ? 0.f : 1.0f / lt;
+  if (p.parts > 1 && wave == 0 && lane < p.tile_rows)
+    p.part_lse[slot * p.tile_rows + lane] = lt == 0.f ? -__builtin_inff() : mref + log2f(lt);
+  float f[16];
+  Columns<D, CAP, BIAS>::per_row(rowv, h, n, fast_exp2(C.m - mref) * inv, f);
+  constexpr int kJ = D / 32;
+  auto at = [&](int dst, int src) {   // outputs of wavefront src for wavefront dst
+    return reinterpret_cast<lds_f32_t*>(smem + (dst * (kWaves - 1) + (src > dst ? src - 1 : src)) * kSwapBytes<D>) +
+           lane * kJ;
+  };
+#pragma unroll
+  for (int d = 0; d < kWaves; ++d)
+    if (d != wave) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int j = 0; j < kJ; ++j) at(d, wave)[e * 64 * kJ + j] = C.o[j][4 * d + e] * f[4 * d + e];
+    }
+  __syncthreads();
+#pragma unroll
+  for (int d = 0; d < kWaves; ++d)
+    if (d == wave) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int r = 8 * d + 4 * h + e;
+        float acc[kJ];
+#pragma unroll
+        for (int j = 0; j < kJ; ++j) {
+          acc[j] = C.o[j][4 * d + e] * f[4 * d + e];
+#pragma unroll
+          for (int w = 0; w < kWaves; ++w)
+            if (w != d) acc[j] += at(d, w)[e * 64 * kJ + j];
+        }
+        const int Rr = row0 + r;
+        if (Rr < rows) {
+          if (p.parts > 1) {
+#pragma unroll
+            for (int j = 0; j < kJ; ++j) store_partial(p.part_o + (slot * p.tile_rows + r) * D + 32 * j + n, acc[j]);
+          } else {
+            uint16_t* dst = p.out + ((size_t)(c.start + Rr / p.group) * p.num_q_heads + g * p.group + Rr % p.group) * D;
+#pragma unroll
+            for (int j = 0; j < kJ; ++j) dst[32 * j + n] = (uint16_t)bf16_rne(acc[j]);
+          }
+        }
+      }
+    }
+}
+
+// Merge of the partitions of one row tile: weights 2^(lse - max lse).
+template <int D>
+__device__ __forceinline__ void merge_body(const BiasedParams& p, int wg) {
+  const int slot0 = wg;
+  const int g = wg % p.num_kv_heads;
+  wg /= p.num_kv_heads;
+  const int tile = wg % p.tiles;
+  const int b = wg / p.tiles;
+  const Chunk c = chunk_of(p, b);
+  const int rows = c.len * p.group;
+  const int row0 = tile * kBiasedTileRows;
+  if (row0 >= rows) return;
+  constexpr int kLanes = D / 4;                       // four dims per thread
+  const int d = 4 * (threadIdx.x % kLanes);
+  const float* lse = p.part_lse + (size_t)slot0 * p.parts * p.tile_rows;
+  const float* po = p.part_o + (size_t)slot0 * p.parts * p.tile_rows * D + d;
+  for (int r = threadIdx.x / kLanes; r < min(kBiasedTileRows, rows - row0); r += 256 / kLanes) {
+    float mx = -__builtin_inff();
+    for (int q = 0; q < p.parts; ++q) mx = fmaxf(mx, lse[q * p.tile_rows + r]);
+    const float mref = mx == -__builtin_inff() ? 0.f : mx;
+    float sum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int q = 0; q < p.parts; ++q) {
+      const float x = lse[q * p.tile_rows + r];
+      if (x == -__builtin_inff()) continue;            // nothing there: its o was not written
+      const float w = fast_exp2(x - mref);
+      const float4 v = *reinterpret_cast<const float4*>(po + (size_t)(q * p.tile_rows + r) * D);
+      sum += w;
+      acc[0] = fmaf(w, v.x, acc[0]);
+      acc[1] = fmaf(w, v.y, acc[1]);
+      acc[2] = fmaf(w, v.z, acc[2]);
+      acc[3] = fmaf(w, v.w, acc[3]);
+    }
+    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+    const int R = row0 + r;
+    uint16_t* dst = p.out + ((size_t)(c.start + R / p.group) * p.num_q_heads + g * p.group + R % p.group) * D + d;
+    *reinterpret_cast<uint2*>(dst) = make_uint2(bf16_rne(acc[0] * inv) | (bf16_rne(acc[1] * inv) << 16),
+                                                bf16_rne(acc[2] * inv) | (bf16_rne(acc[3] * inv) << 16));
+  }
+}
+
+}  // namespace biased
+}  // namespace pa

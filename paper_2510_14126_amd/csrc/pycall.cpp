@@ -15,6 +15,7 @@
 #include <Python.h>
 
 #include "paged_attn.h"
+#include "paged_attn_ops.h"
 
 #include <cstdint>
 #include <tuple>
@@ -121,8 +122,14 @@ const Entry kEntries[] = {
     PA_ENTRY(10, paged_attn_decode_cascade_append),
     PA_ENTRY(11, paged_attn_decode_noalloc),
     PA_ENTRY(12, paged_attn_extend),
+    // paged_attn_ops.h
+    PA_ENTRY(13, paged_attn_norm_rope),
+    PA_ENTRY(14, paged_attn_rope_append),
+    PA_ENTRY(15, paged_attn_decode_biased),
+    PA_ENTRY(16, paged_attn_extend_biased),
 };
 constexpr int kNumEntries = sizeof kEntries / sizeof kEntries[0];
+constexpr int kNumDecode = 13;   // those of paged_attn.h, NAMES; the others are OPS_NAMES
 
 // bind({name: (address, ctypes call)}): every function above must be given.
 PyObject* bind(PyObject*, PyObject* calls) {
@@ -156,11 +163,15 @@ PyMODINIT_FUNC PyInit__pycall(void) {
   g_data_ptr = PyUnicode_InternFromString("data_ptr");
   PyObject* m = g_data_ptr ? PyModule_Create(&g_module) : nullptr;
   if (!m) return nullptr;
-  PyObject* names = PyTuple_New(kNumEntries);
-  for (int i = 0; names && i < kNumEntries; ++i)
-    PyTuple_SET_ITEM(names, i, PyUnicode_FromString(kEntries[i].name));
-  if (!names || PyModule_AddObject(m, "NAMES", names) < 0) {
+  auto add_names = [&](const char* as, int from, int to) {
+    PyObject* names = PyTuple_New(to - from);
+    for (int i = from; names && i < to; ++i)
+      PyTuple_SET_ITEM(names, i - from, PyUnicode_FromString(kEntries[i].name));
+    if (names && PyModule_AddObject(m, as, names) == 0) return true;
     Py_XDECREF(names);
+    return false;
+  };
+  if (!add_names("NAMES", 0, kNumDecode) || !add_names("OPS_NAMES", kNumDecode, kNumEntries)) {
     Py_DECREF(m);
     return nullptr;
   }
