@@ -236,17 +236,48 @@ namespace {
 
 constexpr double kLog2e = 1.4426950408889634;
 
-// Partitions: enough workgroups to fill the GPU.
+// How a call's rows and tokens are dealt to workgroups.
+//
+// Rows: 128 per workgroup over one stream of its tokens (big), or 32 whose
+// tokens its wavefronts split, a chain four times shorter per workgroup: while
+// those, weighed by the tokens a chunk's average row sees against the longest
+// context, are all resident at once (two per CU), or while they are at most
+// twice the others, whose tiles are then mostly empty.  32-row / 128-row form,
+// 32 heads over 8, capped scores: one chunk of 16 over 2320 tokens 13 / 96 us,
+// of 256 over 2560 39 / 106, eight of 64 over 2368 62 / 102; three of 600 over
+// 2904 (1800 workgroups) 189 / 155, one prompt of 8191 1140 / 881.
+//
+// Tokens of a 32-row tile: one partition, or several, merged by a second launch
+// (2.5 us), where the tiles alone are fewer workgroups than CUs and hold more
+// than kWholeBlocks blocks each.  One / several partitions, decode, 32 heads over
+// 8: one sequence of 512 tokens 7.0 / 8.7 us, 768 8.9 / 8.5, 1024 10.9 / 8.6;
+// twice as many workgroups: one of 30011 28.0 / 28.0, eight of 4096 23.9 / 26.0.
+// In a decode, whose contexts differ, a partition holds at most kMostBlocks: 256
+// of 64..8192 tokens in partitions of at most 64 / 96 / 128 blocks 269 / 265 / 265
+// us, 64 with a window of 4096 169 / 168 / 167, of 32 blocks 303 / 175.
+constexpr int64_t kFillWorkgroups = 256;
+constexpr int64_t kWholeBlocks = 40, kLeastBlocks = 16, kMostBlocks = 128;
 pa::BiasedPlan biased_plan(int batch, int num_kv_heads, int group, int max_ctx, int max_chunk, int window) {
   pa::BiasedPlan pl;
   const int64_t rows = (int64_t)std::max(max_chunk, 1) * group;
-  pl.tiles = (int32_t)((rows + pa::kBiasedTileRows - 1) / pa::kBiasedTileRows);
+  const int64_t tiles = (rows + pa::kBiasedTileRows - 1) / pa::kBiasedTileRows;
+  const int64_t big_tiles = (rows + pa::kBiasedWgRows - 1) / pa::kBiasedWgRows;
+  const int64_t wgs = std::max<int64_t>(1, batch * tiles * num_kv_heads), big_wgs = batch * big_tiles * num_kv_heads;
+  pl.big = max_chunk > 1 && wgs > 2 * big_wgs &&
+           wgs * (2.0 * max_ctx - max_chunk) > 2.0 * 2 * kFillWorkgroups * max_ctx;
+  pl.tiles = (int32_t)(pl.big ? big_tiles : tiles);
   pl.tile_rows = (int32_t)std::min<int64_t>(rows, pa::kBiasedTileRows);
-  pl.min_blocks = 16;
-  const int64_t span = window > 0 ? std::min<int64_t>(max_ctx, (int64_t)window + pa::kBiasedTileRows / group + 1) : max_ctx;
-  const int64_t most = std::max<int64_t>(1, (span + 16 * pl.min_blocks - 1) / (16 * pl.min_blocks));
-  const int64_t wgs = std::max<int64_t>(1, (int64_t)batch * pl.tiles * num_kv_heads);
-  pl.parts = (int32_t)std::min(most, std::max<int64_t>(1, 2048 / wgs));
+  const int64_t all = ((int64_t)max_ctx + PA_BLOCK_SIZE - 1) / PA_BLOCK_SIZE;
+  // a window spans its own tokens and those between a tile's first and last row, wherever they begin in a block
+  const int64_t blocks = window > 0 ? std::min(all, ((int64_t)window + pa::kBiasedTileRows / group + PA_BLOCK_SIZE - 1) / PA_BLOCK_SIZE + 1) : all;
+  int64_t per = blocks;
+  if (!pl.big && blocks > kWholeBlocks) {
+    per = std::max(kLeastBlocks, (blocks * wgs / kFillWorkgroups + 1) / 2 * 2);
+    if (max_chunk <= 1) per = std::min(per, kMostBlocks);
+  }
+  per = std::max<int64_t>(per, 1);
+  pl.parts = (int32_t)std::max<int64_t>(1, (blocks + per - 1) / per);
+  pl.part_blocks = (int32_t)std::min<int64_t>(per, 0x7fffffff);
   return pl;
 }
 
@@ -270,7 +301,7 @@ int plan_biased(const pa_kv_pool* pool, int32_t batch, int32_t num_q_heads, int3
     return fail(PA_EINVAL, "%s: max_chunk = %d outside [0, max_context_len = %d]", fn, max_chunk, max_context_len);
   if (window < 0) return fail(PA_EINVAL, "%s: window = %d < 0", fn, window);
   const int32_t group = num_q_heads / pool->num_kv_heads;
-  const int64_t rows = (int64_t)max_chunk * group;
+  const int64_t rows = (int64_t)std::max(max_chunk, 1) * group;
   if (rows > 0x7fffffffLL) return fail(PA_EINVAL, "%s: max_chunk * heads per KV head = %lld is too large", fn, (long long)rows);
   const int64_t tiles = (rows + pa::kBiasedTileRows - 1) / pa::kBiasedTileRows;
   *slots = (int64_t)batch * tiles;
@@ -334,10 +365,12 @@ int biased_impl(const pa_kv_pool* pool, const void* q, const int32_t* q_start, i
   p.max_chunk = max_chunk;
   p.total_q = total_q;
   p.window = window;
+  p.big = pl.big;
   p.tiles = pl.tiles;
   p.parts = pl.parts;
-  p.min_blocks = pl.min_blocks;
+  p.part_blocks = pl.part_blocks;
   p.tile_rows = pl.tile_rows;
+  p.stream_tiles = !q_start && pl.tiles == 1 && pool->shared_blocks == 0;
   p.scale_log2 = (float)(scale * kLog2e);
   if (softcap > 0.f) {
     // tanh(z) / z on |z| <= 1/2 as a polynomial in z^2, z = raw * |scale| / softcap

@@ -1,31 +1,70 @@
 // Attention with capped, biased or masked scores over the paged cache: kernel
 // entry points.  The algorithms live in biased_body.h.
 #include "biased_body.h"
+#include "biased_decode.h"
 
 namespace pa {
 namespace {
 
 using mfma::kWaves;
 
-template <int D, bool CAP, bool BIAS>
+template <int D, bool CAP, bool BIAS, int AUX>
 __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 8)))
 biased_split_kernel(const BiasedParams p) {
   __shared__ __attribute__((aligned(16))) uint8_t smem[biased::kSplitLdsBytes<D>];
-  biased::split_body<D, CAP, BIAS>(p, blockIdx.x, (lds_u8_t*)smem);
+  biased::split_body<D, CAP, BIAS, AUX>(p, blockIdx.x, (lds_u8_t*)smem);
 }
 
-template <int D>
-__global__ void __launch_bounds__(256) biased_merge_kernel(const BiasedParams p) {
-  biased::merge_body<D>(p, blockIdx.x);
+template <int D, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 8)))
+biased_big_kernel(const BiasedParams p) {
+  __shared__ __attribute__((aligned(16))) uint8_t smem[biased::kBigLdsBytes<D>];
+  biased::big_body<D, CAP, BIAS>(p, blockIdx.x, (lds_u8_t*)smem);
+}
+
+template <int D, int GP, bool CAP, bool BIAS, int AUX>
+__global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 8)))
+biased_decode_kernel(const BiasedParams p) {
+  __shared__ __attribute__((aligned(16))) uint8_t smem[biased::kDecodeLdsBytes<D, GP>];
+  biased::decode_body<D, GP, CAP, BIAS, AUX>(p, blockIdx.x, (lds_u8_t*)smem);
+}
+
+// One row per workgroup (NW = 4 wavefronts on it), or four (NW = 1).
+template <int D, int NW>
+__global__ void __launch_bounds__(64 * kWaves) biased_merge_kernel(const BiasedParams p) {
+  __shared__ __attribute__((aligned(16))) float smem[NW > 1 ? NW * (D + 1) : 1];
+  const int wave = wave_uniform(threadIdx.x >> 6);
+  const int64_t row = NW > 1 ? blockIdx.x : (int64_t)blockIdx.x * kWaves + wave;
+  if (row >= (int64_t)p.batch * p.tiles * p.num_kv_heads * p.tile_rows) return;
+  biased::merge_body<D, NW>(p, (int)(row / p.tile_rows), (int)(row % p.tile_rows), NW > 1 ? wave : 0, (lds_f32_t*)smem);
 }
 
 template <int D, bool CAP, bool BIAS>
 hipError_t launch_t(const BiasedParams& p, hipStream_t stream) {
   const int64_t tiles = (int64_t)p.batch * p.tiles * p.num_kv_heads;
-  hipLaunchKernelGGL((biased_split_kernel<D, CAP, BIAS>), dim3((unsigned)(tiles * p.parts)), dim3(64 * kWaves), 0,
-                     stream, p);
-  if (p.parts > 1)
-    hipLaunchKernelGGL(biased_merge_kernel<D>, dim3((unsigned)tiles), dim3(256), 0, stream, p);
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(tiles * p.parts)), dim3(64 * kWaves), 0, stream, p);
+  };
+  if (!p.q_start && p.group <= 4)
+    go(p.stream_tiles ? biased_decode_kernel<D, 4, CAP, BIAS, kLoadStreaming>
+                      : biased_decode_kernel<D, 4, CAP, BIAS, kLoadDefault>);
+  else if (!p.q_start && p.group <= 8)
+    go(p.stream_tiles ? biased_decode_kernel<D, 8, CAP, BIAS, kLoadStreaming>
+                      : biased_decode_kernel<D, 8, CAP, BIAS, kLoadDefault>);
+  else if (p.big)
+    go(biased_big_kernel<D, CAP, BIAS>);
+  else if (p.stream_tiles)
+    go(biased_split_kernel<D, CAP, BIAS, kLoadStreaming>);
+  else
+    go(biased_split_kernel<D, CAP, BIAS, kLoadDefault>);
+  if (p.parts > 1) {
+    const int64_t rows = tiles * p.tile_rows;
+    if (p.parts > biased::kGroup && rows <= 512)
+      hipLaunchKernelGGL((biased_merge_kernel<D, kWaves>), dim3((unsigned)rows), dim3(64 * kWaves), 0, stream, p);
+    else
+      hipLaunchKernelGGL((biased_merge_kernel<D, 1>), dim3((unsigned)((rows + kWaves - 1) / kWaves)), dim3(64 * kWaves),
+                         0, stream, p);
+  }
   return hipGetLastError();
 }
 

@@ -134,6 +134,19 @@ __device__ __forceinline__ Row row_of(const BiasedParams& p, const Chunk& c, int
   return r;
 }
 
+// A raw score capped, in log2 units; far: some score of the stage is beyond the
+// polynomial (wave-uniform).
+__device__ __forceinline__ float cap_score(const BiasedParams& p, float x, bool far) {
+  const float u = x * x;
+  float y = x * fmaf(u, fmaf(u, fmaf(u, p.c3, p.c2), p.c1), p.c0);
+  if (far) {
+    const float t = fast_exp2(x * p.two_z);
+    const float z = fmaf(-2.f * p.cap, __builtin_amdgcn_rcpf(t + 1.f), p.cap);
+    y = fabsf(x) <= p.raw_max ? y : z;
+  }
+  return y;
+}
+
 // The 32 columns of one wavefront: queries (Q^T operand of step s: dims 16s + 8h
 // .. of column n), softmax state, outputs.
 template <int D, bool CAP, bool BIAS>
@@ -187,16 +200,7 @@ struct Columns {
       for (int r = 0; r < 16; ++r) most = fmaxf(most, fabsf(a[r]));
       const bool far = __builtin_amdgcn_ballot_w64(!(most <= p.raw_max)) != 0;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float x = a[r], u = x * x;
-        float y = x * fmaf(u, fmaf(u, fmaf(u, p.c3, p.c2), p.c1), p.c0);
-        if (far) {
-          const float t = fast_exp2(x * p.two_z);
-          const float z = fmaf(-2.f * p.cap, __builtin_amdgcn_rcpf(t + 1.f), p.cap);
-          y = fabsf(x) <= p.raw_max ? y : z;
-        }
-        a[r] = y;
-      }
+      for (int r = 0; r < 16; ++r) a[r] = cap_score(p, a[r], far);
     }
     if constexpr (BIAS) {
       const float d0 = row.pos - (float)(t0 + 4 * h);
@@ -306,9 +310,9 @@ struct Columns {
 
   // Adds what stood in V where a masked stage was given zeros for infinities and
   // NaN, to the rows that see it (its weight is above 0: it makes them infinite
-  // or NaN).  st: the stage's V as it is, first token t0.  rowv: 32 floats of LDS
+  // or NaN).  v: the stage's V as it is, first token t0.  rowv: 32 floats of LDS
   // of the wavefront's own.
-  __device__ __forceinline__ void add_special(int t0, const lds_u8_t* st, lds_f32_t* rowv, int h, int n) {
+  __device__ __forceinline__ void add_special(int t0, const lds_u8_t* v, lds_f32_t* rowv, int h, int n) {
     float from[16], to[16];
     per_row(rowv, h, n, __int_as_float(row.lo), from);
     per_row(rowv, h, n, __int_as_float(row.hi), to);
@@ -316,12 +320,11 @@ struct Columns {
     for (int j = 0; j < D / 32; ++j) {
 #pragma unroll 1
       for (int t = 0; t < kTokens; ++t) {
-        const uint32_t x = *reinterpret_cast<const lds_u16_t*>(st + kVOffset<D> + v_off<D>(t, (32 * j + n) >> 3) +
-                                                               ((n & 7) << 1));
-        const float v = (x & 0x7f80u) == 0x7f80u ? bf16_lo(x) : 0.f;
+        const uint32_t x = *reinterpret_cast<const lds_u16_t*>(v + v_off<D>(t, (32 * j + n) >> 3) + ((n & 7) << 1));
+        const float y = (x & 0x7f80u) == 0x7f80u ? bf16_lo(x) : 0.f;
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          if (t0 + t >= __float_as_int(from[r]) && t0 + t < __float_as_int(to[r])) o[j][r] += v;
+          if (t0 + t >= __float_as_int(from[r]) && t0 + t < __float_as_int(to[r])) o[j][r] += y;
       }
     }
   }
@@ -332,6 +335,35 @@ __device__ __forceinline__ uint32_t finite_part(uint32_t x, uint32_t& odd) {
   const uint32_t bad = (((x & 0x7f807f80u) + 0x00800080u) >> 15) & 0x00010001u;   // an exponent of all ones carries
   odd |= bad;
   return x & ~(bad * 0xffffu);
+}
+
+// add_special over the masked stages (from, from + step, ...) of cnt blocks that
+// begin at block j0 with table entries bt: all lanes of a wavefront, for its own
+// columns.  v: LDS for a stage's V of the wavefront's own.
+template <int D, typename C>
+__device__ __forceinline__ void special_pass(C& cols, const BiasedParams& p, const int32_t* bt, const uint16_t* vbase,
+                                             int cnt, int j0, int from, int step, int all_lo, int all_hi, lds_u8_t* v,
+                                             lds_f32_t* rowv) {
+  constexpr int kChunks = D / 8;
+  const int lane = threadIdx.x & 63;
+#pragma unroll 1
+  for (int s = from; 2 * s < cnt; s += step) {
+    const int t0 = (j0 + 2 * s) * 16;
+    if (t0 >= all_lo && t0 + kTokens <= all_hi) continue;
+#pragma unroll 1
+    for (int r = lane / kChunks; r < kTokens; r += 64 / kChunks) {
+      const int j = 2 * s + (r >> 4);
+      uint4 x = make_uint4(0, 0, 0, 0);
+      if (j < cnt) {
+        const size_t id = (size_t)min(max(bt[j], 0), p.num_blocks - 1);
+        x = *reinterpret_cast<const uint4*>(vbase + id * p.num_kv_heads * (16 * D) + (r & 15) * D + lane % kChunks * 8);
+      }
+      *reinterpret_cast<lds_u32x4_t*>(v + v_off<D>(r, lane % kChunks)) = u32x4_t{x.x, x.y, x.z, x.w};
+    }
+    __builtin_amdgcn_wave_barrier();
+    cols.add_special(t0, v, rowv, lane >> 5, lane & 31);
+    __builtin_amdgcn_wave_barrier();
+  }
 }
 
 // --------------------------------------------------------------------------
@@ -345,7 +377,12 @@ template <int D> constexpr int kSplitLdsBytes = kSplitQuery<D> + kBiasedTileRows
 static_assert(kWaves * (kWaves - 1) * kSwapBytes<128> <= kSplitStats<128>, "the merge reuses the stages");
 static_assert(kWaves * (kWaves - 1) * kSwapBytes<64> <= kSplitStats<64>, "the merge reuses the stages");
 
-template <int D, bool CAP, bool BIAS>
+// In place of the log-sum-exp of a row tile's first partition: it was the only
+// one and the output is written.  (A row's own is at most finite, or NaN.)
+constexpr float kWhole = __builtin_inff();
+
+// AUX: cache policy of the tiles' loads.
+template <int D, bool CAP, bool BIAS, int AUX>
 __device__ __forceinline__ void split_body(const BiasedParams& p, int wg, lds_u8_t* smem) {
   constexpr int kRows = kBiasedTileRows;
   const int lane = threadIdx.x & 63;
@@ -360,6 +397,14 @@ __device__ __forceinline__ void split_body(const BiasedParams& p, int wg, lds_u8
   const int b = wg % p.batch;
   const int part = wg / p.batch;
 
+  // Where nothing but the context length bounds what rows see, the partition's
+  // first block ids are loaded with it instead of after it.
+  const bool whole = p.window == 0 && p.first_tokens == nullptr;
+  int ids_first = 0;
+  if (whole) {
+    const int64_t j = (int64_t)part * p.part_blocks + lane;
+    ids_first = p.block_tables[(size_t)b * p.bt_stride + min(j, (int64_t)p.bt_stride - 1)];
+  }
   const Chunk c = chunk_of(p, b);
   const int rows = c.len * p.group;
   const int row0 = tile * kRows;
@@ -383,10 +428,11 @@ __device__ __forceinline__ void split_body(const BiasedParams& p, int wg, lds_u8
   // This partition's blocks.
   const int first = lo >> 4;
   const int nblk = hi > lo ? ((hi + 15) >> 4) - first : 0;
-  const int per = p.parts == 1 ? nblk : max(p.min_blocks, ((nblk + p.parts - 1) / p.parts + 1) & ~1);
+  const int per = p.parts == 1 ? nblk : p.part_blocks;
   const int j0 = first + part * per;
   const int cnt = min(per, nblk - part * per);          // <= 0: nothing in this partition
   const size_t slot = (((size_t)b * p.tiles + tile) * p.num_kv_heads + g) * p.parts + part;
+  const bool split = p.parts > 1 && nblk > per;         // else the first partition writes the output
   if (cnt <= 0 && p.parts > 1) {
     if (threadIdx.x < p.tile_rows) p.part_lse[slot * p.tile_rows + threadIdx.x] = -__builtin_inff();
     return;
@@ -426,7 +472,8 @@ __device__ __forceinline__ void split_body(const BiasedParams& p, int wg, lds_u8
     const int j = 64 * chunk + lane;
     return j < cnt ? min(max(bt[j], 0), p.num_blocks - 1) : 0;
   };
-  int ids = ids_of(0), ids_next = ids_of(1), chunk = 0;
+  int ids = whole ? (lane < cnt ? min(max(ids_first, 0), p.num_blocks - 1) : 0) : ids_of(0);
+  int ids_next = ids_of(1), chunk = 0;
   auto load = [&](int s) {
     if (2 * s >> 6 != chunk) {                            // uniform; a wavefront's stages skip no chunk
       ids = ids_next;
@@ -444,8 +491,8 @@ __device__ __forceinline__ void split_body(const BiasedParams& p, int wg, lds_u8
           const_cast<uint16_t*>(vbase + (size_t)id[e] * blk_stride), 0, bytes, kBufferDescWord3);
 #pragma unroll
       for (int i = 0; i < kLoads / 2; ++i) {
-        rk[e * kLoads / 2 + i] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(dk, lane_off + i * 1024, 0, 0));
-        rv[e * kLoads / 2 + i] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(dv, lane_off + i * 1024, 0, 0));
+        rk[e * kLoads / 2 + i] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(dk, lane_off + i * 1024, 0, AUX));
+        rv[e * kLoads / 2 + i] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(dv, lane_off + i * 1024, 0, AUX));
       }
     }
   };
@@ -486,26 +533,8 @@ __device__ __forceinline__ void split_body(const BiasedParams& p, int wg, lds_u8
     C.attend(a, st, lane);
   }
 
-  if (__builtin_amdgcn_ballot_w64(odd != 0) != 0) {
-#pragma unroll 1
-    for (int s = wave; s < nstage; s += kWaves) {
-      const int t0 = (j0 + 2 * s) * 16;
-      if (t0 >= all_lo && t0 + kTokens <= all_hi) continue;
-#pragma unroll 1
-      for (int r = lrow; r < kTokens; r += kRowsPerLoad) {
-        const int j = 2 * s + (r >> 4);
-        uint4 x = make_uint4(0, 0, 0, 0);
-        if (j < cnt) {
-          const size_t id = (size_t)min(max(bt[j], 0), p.num_blocks - 1);
-          x = *reinterpret_cast<const uint4*>(vbase + id * blk_stride + (r & 15) * D + lchunk * 8);
-        }
-        *reinterpret_cast<lds_u32x4_t*>(st + kVOffset<D> + v_off<D>(r, lchunk)) = u32x4_t{x.x, x.y, x.z, x.w};
-      }
-      __builtin_amdgcn_wave_barrier();
-      C.add_special(t0, st, rowv, h, n);
-      __builtin_amdgcn_wave_barrier();
-    }
-  }
+  if (__builtin_amdgcn_ballot_w64(odd != 0) != 0)
+    special_pass<D>(C, p, bt, vbase, cnt, j0, wave, kWaves, all_lo, all_hi, st, rowv);
 
   // Merge.  Row n's maximum and sum over the wavefronts, then each wavefront
   // scales its outputs to the common maximum and the final sum; wavefront d
@@ -528,7 +557,7 @@ __device__ __forceinline__ void split_body(const BiasedParams& p, int wg, lds_u8
   for (int w = 0; w < kWaves; ++w) lt = fmaf(sl[w * kRows + n], fast_exp2(sm[w * kRows + n] - mref), lt);
   const float inv = lt == 0.f ? 0.f : 1.0f / lt;
   if (p.parts > 1 && wave == 0 && lane < p.tile_rows)
-    p.part_lse[slot * p.tile_rows + lane] = lt == 0.f ? -__builtin_inff() : mref + log2f(lt);
+    p.part_lse[slot * p.tile_rows + lane] = !split ? kWhole : (lt == 0.f ? -__builtin_inff() : mref + log2f(lt));
   float f[16];
   Columns<D, CAP, BIAS>::per_row(rowv, h, n, fast_exp2(C.m - mref) * inv, f);
   constexpr int kJ = D / 32;
@@ -561,7 +590,7 @@ __device__ __forceinline__ void split_body(const BiasedParams& p, int wg, lds_u8
         }
         const int Rr = row0 + r;
         if (Rr < rows) {
-          if (p.parts > 1) {
+          if (split) {
 #pragma unroll
             for (int j = 0; j < kJ; ++j) store_partial(p.part_o + (slot * p.tile_rows + r) * D + 32 * j + n, acc[j]);
           } else {
@@ -574,44 +603,278 @@ __device__ __forceinline__ void split_body(const BiasedParams& p, int wg, lds_u8
     }
 }
 
-// Merge of the partitions of one row tile: weights 2^(lse - max lse).
-template <int D>
-__device__ __forceinline__ void merge_body(const BiasedParams& p, int wg) {
-  const int slot0 = wg;
+// --------------------------------------------------------------------------
+// 128 rows per workgroup, 32 per wavefront, over one stream of stages through
+// LDS that all of them read: for long chunks.
+//
+// The loop is software-pipelined by one stage: iteration j computes the scores
+// of stage j+1, the weights of stage j and their PV, publishes stage j+2 to LDS
+// and loads stage j+3; every slot is read only between the barriers that follow
+// its writing and precede its next writing.
+// --------------------------------------------------------------------------
+constexpr int kSlots = 3;
+template <int D> constexpr int kBigRow = kSlots * kStageBytes<D>;         // one value per row, per wavefront
+template <int D> constexpr int kBigRange = kBigRow<D> + kWaves * kBiasedTileRows * 4;   // ranges of the wavefronts
+template <int D> constexpr int kBigLdsBytes = kBigRange<D> + 4 * kWaves * 4;
+static_assert(kWaves * kBiasedTileRows * 128 * 2 <= kBigRow<128> && kWaves * kBiasedTileRows * 64 * 2 <= kBigRow<64>,
+              "the stages' room holds the outputs, and a V tile per wavefront");
+
+template <int D, bool CAP, bool BIAS>
+__device__ __forceinline__ void big_body(const BiasedParams& p, int wg, lds_u8_t* smem) {
+  const int lane = threadIdx.x & 63;
+  const int wave = wave_uniform(threadIdx.x >> 6);
+  const int h = lane >> 5;
+  const int n = lane & 31;
+
+  const int g = wg % p.num_kv_heads;
+  wg /= p.num_kv_heads;
+  // A chunk's last rows see the most tokens: they start first.
+  const int tile = p.tiles - 1 - wg % p.tiles;
+  const int b = wg / p.tiles;
+  const Chunk c = chunk_of(p, b);
+  const int rows = c.len * p.group;
+  if (tile * kBiasedWgRows >= rows) return;            // whole workgroup: no rows here
+  const int row0 = tile * kBiasedWgRows + kBiasedTileRows * wave;
+
+  // A column without a row repeats the workgroup's first and is not written.
+  const int R = row0 + n < rows ? row0 + n : tile * kBiasedWgRows;
+  const Row row = row_of<BIAS>(p, c, b, g, R);
+  int lo, hi, all_lo, all_hi;                          // tokens that some row, that every row of the workgroup sees
+  {
+    const bool none = row.hi <= row.lo;
+    lds_i32_t* range = reinterpret_cast<lds_i32_t*>(smem + kBigRange<D>);
+    const int x[4] = {-min32(none ? 0x3fffffff : row.lo), max32(none ? 0 : row.hi), max32(row.lo),
+                      -min32(none ? 0 : row.hi)};
+    if (lane < 4) range[4 * wave + lane] = lane == 0 ? x[0] : (lane == 1 ? x[1] : (lane == 2 ? x[2] : x[3]));
+    __syncthreads();
+    int y[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      y[i] = range[i];
+#pragma unroll
+      for (int w = 1; w < kWaves; ++w) y[i] = max(y[i], range[4 * w + i]);
+      y[i] = wave_uniform(y[i]);
+    }
+    lo = -y[0];
+    hi = y[1];
+    all_lo = y[2];
+    all_hi = -y[3];
+    __syncthreads();                                   // `range` is used again
+  }
+  const int j0 = lo >> 4;
+  const int cnt = hi > lo ? ((hi + 15) >> 4) - j0 : 0;
+
+  Columns<D, CAP, BIAS> C;
+  C.init(p, row);
+  u32x4_t q[D / 16];
+  {
+    const uint16_t* q_row = p.q + ((size_t)(c.start + R / p.group) * p.num_q_heads + g * p.group + R % p.group) * D;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) q[s] = C.query(p, q_row, s, h);
+  }
+  auto query = [&](int s) { return q[s]; };
+
+  constexpr size_t kTile = 16 * D;
+  const size_t blk_stride = (size_t)p.num_kv_heads * kTile;
+  const uint16_t* kbase = p.k_pool + (size_t)g * kTile;
+  const uint16_t* vbase = p.v_pool + (size_t)g * kTile;
+  const int32_t* bt = p.block_tables + (size_t)b * p.bt_stride + j0;
+  auto ids_of = [&](int chunk) {
+    const int j = 64 * chunk + lane;
+    return j < cnt ? min(max(bt[j], 0), p.num_blocks - 1) : 0;
+  };
+  int ids = ids_of(0), ids_next = ids_of(1), chunk = 0;
+
+  // The workgroup's share of a stage: 256 threads take 16 bytes each of K and V,
+  // D / 64 times: whole blocks (D = 128) or both halves at once (D = 64).
+  constexpr int kLoads = D / 64;
+  constexpr int kChunks = D / 8;
+  const int lrow = threadIdx.x / kChunks, lchunk = threadIdx.x % kChunks;
+  const int lane_off = (D == 128 ? threadIdx.x : threadIdx.x & 127) * 16;
+  u32x4_t rk[kLoads], rv[kLoads];
+  auto load = [&](int s) {
+    if (2 * s >> 6 != chunk) {                         // uniform
+      ids = ids_next;
+      ids_next = ids_of(++chunk + 1);
+    }
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int j = 2 * s + (D == 128 ? i : wave >> 1);
+      const size_t id = (size_t)__builtin_amdgcn_readlane(ids, j & 63);
+      const int bytes = j < cnt ? (int)kTile * 2 : 0;  // none past the last block: zeros
+      const __amdgpu_buffer_rsrc_t dk = __builtin_amdgcn_make_buffer_rsrc(
+          const_cast<uint16_t*>(kbase + id * blk_stride), 0, bytes, kBufferDescWord3);
+      const __amdgpu_buffer_rsrc_t dv = __builtin_amdgcn_make_buffer_rsrc(
+          const_cast<uint16_t*>(vbase + id * blk_stride), 0, bytes, kBufferDescWord3);
+      rk[i] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(dk, lane_off, 0, 0));
+      rv[i] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(dv, lane_off, 0, 0));
+    }
+  };
+  auto first_of = [&](int s) { return (j0 + 2 * s) * 16; };
+  auto edge = [&](int s) { return first_of(s) < all_lo || first_of(s) + kTokens > all_hi; };
+  uint32_t odd = 0;                                    // infinities or NaN among V where there are masks
+  auto publish = [&](int s, int slot) {
+    if (edge(s)) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int t = first_of(s) + 16 * i + lrow;
+        if (t < lo || t >= hi) {
+          rk[i] = u32x4_t{0, 0, 0, 0};
+          rv[i] = u32x4_t{0, 0, 0, 0};
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) rv[i][e] = finite_part(rv[i][e], odd);
+      }
+    }
+    lds_u8_t* st = smem + slot * kStageBytes<D>;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      *reinterpret_cast<lds_u32x4_t*>(st + k_off<D>(16 * i + lrow, lchunk)) = rk[i];
+      *reinterpret_cast<lds_u32x4_t*>(st + kVOffset<D> + v_off<D>(16 * i + lrow, lchunk)) = rv[i];
+    }
+  };
+  lds_f32_t* rowv = reinterpret_cast<lds_f32_t*>(smem + kBigRow<D>) + wave * kBiasedTileRows;
+
+  const int nstage = (cnt + 1) >> 1;
+  load(0);
+  publish(0, 0);
+  load(1);
+  publish(1, 1);
+  load(2);
+  __syncthreads();
+  floatx16_t a = C.scores(smem, h, n, query);
+  C.shape(p, a, first_of(0), edge(0), h);
+  C.raise(a, rowv, h, n);
+  for (int s0 = 0; s0 < nstage; s0 += kSlots) {
+#pragma unroll
+    for (int u = 0; u < kSlots; ++u) {
+      const int s = s0 + u;
+      if (s < nstage) {                                // uniform over the workgroup
+        floatx16_t next = C.scores(smem + (u + 1) % kSlots * kStageBytes<D>, h, n, query);
+        publish(s + 2, (u + 2) % kSlots);
+        load(s + 3);
+        C.attend(a, smem + u * kStageBytes<D>, lane);
+        if (s + 1 < nstage) {
+          C.shape(p, next, first_of(s + 1), edge(s + 1), h);
+          C.raise(next, rowv, h, n);
+        }
+        a = next;
+        __syncthreads();
+      }
+    }
+  }
+
+  // Every wavefront is past the last barrier: the stages are free.
+  {
+    lds_i32_t* flag = reinterpret_cast<lds_i32_t*>(smem + kBigRange<D>);
+    if (lane == 0) flag[wave] = 0;
+    if (__builtin_amdgcn_ballot_w64(odd != 0) != 0 && lane == 0) flag[wave] = 1;
+    __syncthreads();
+    if (wave_uniform(flag[0] | flag[1] | flag[2] | flag[3]) != 0)
+      special_pass<D>(C, p, bt, vbase, cnt, j0, 0, 1, all_lo, all_hi, smem + wave * (kBiasedTileRows * D * 2), rowv);
+  }
+
+  // Normalise, transpose through LDS and write bf16 rows in 16-byte pieces.
+  float lx = C.l, ly = C.l;
+  swap32(lx, ly);
+  const float lcol = lx + ly;
+  float inv[16];
+  Columns<D, CAP, BIAS>::per_row(rowv, h, n, lcol == 0.f ? 0.f : 1.0f / lcol, inv);
+  lds_u8_t* out = smem + wave * (kBiasedTileRows * D * 2);
+#pragma unroll
+  for (int r = 0; r < 16; ++r)
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j)
+      *reinterpret_cast<lds_u16_t*>(out + (8 * (r >> 2) + 4 * h + (r & 3)) * (D * 2) + (32 * j + n) * 2) =
+          (uint16_t)bf16_rne(C.o[j][r] * inv[r]);
+  __builtin_amdgcn_wave_barrier();
+  constexpr int kRowsPerStore = 64 / kChunks;
+#pragma unroll
+  for (int i = 0; i < kBiasedTileRows / kRowsPerStore; ++i) {
+    const int r = row0 + kRowsPerStore * i + lane / kChunks;
+    const u32x4_t x = *reinterpret_cast<const lds_u32x4_t*>(out + i * 1024 + lane * 16);
+    if (r < rows)
+      *reinterpret_cast<u32x4_t*>(p.out + ((size_t)(c.start + r / p.group) * p.num_q_heads + g * p.group + r % p.group) * D +
+                                  lane % kChunks * 8) = x;
+  }
+}
+
+// Merge of the partitions of row `r` of a row tile: weights 2^(lse - max lse),
+// NW wavefronts per row, D / 64 dims per lane.  Lane q loads lse_q (64
+// partitions per round); the rows of the partitions that hold something are
+// dealt to the wavefronts in groups of kGroup that are loaded together, and the
+// wavefronts' sums are added in order through LDS.
+constexpr int kGroup = 8;
+template <int D, int NW>
+__device__ __forceinline__ void merge_body(const BiasedParams& p, int slot0, int r, int wave, lds_f32_t* smem) {
+  constexpr int DPL = D / 64;
+  const int lane = threadIdx.x & 63;
+  int wg = slot0;
   const int g = wg % p.num_kv_heads;
   wg /= p.num_kv_heads;
   const int tile = wg % p.tiles;
   const int b = wg / p.tiles;
+  const float* lse = p.part_lse + (size_t)slot0 * p.parts * p.tile_rows + r;
+  const float x0 = lane < p.parts ? lse[lane * p.tile_rows] : -__builtin_inff();
   const Chunk c = chunk_of(p, b);
-  const int rows = c.len * p.group;
-  const int row0 = tile * kBiasedTileRows;
-  if (row0 >= rows) return;
-  constexpr int kLanes = D / 4;                       // four dims per thread
-  const int d = 4 * (threadIdx.x % kLanes);
-  const float* lse = p.part_lse + (size_t)slot0 * p.parts * p.tile_rows;
-  const float* po = p.part_o + (size_t)slot0 * p.parts * p.tile_rows * D + d;
-  for (int r = threadIdx.x / kLanes; r < min(kBiasedTileRows, rows - row0); r += 256 / kLanes) {
-    float mx = -__builtin_inff();
-    for (int q = 0; q < p.parts; ++q) mx = fmaxf(mx, lse[q * p.tile_rows + r]);
-    const float mref = mx == -__builtin_inff() ? 0.f : mx;
-    float sum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int q = 0; q < p.parts; ++q) {
-      const float x = lse[q * p.tile_rows + r];
-      if (x == -__builtin_inff()) continue;            // nothing there: its o was not written
-      const float w = fast_exp2(x - mref);
-      const float4 v = *reinterpret_cast<const float4*>(po + (size_t)(q * p.tile_rows + r) * D);
-      sum += w;
-      acc[0] = fmaf(w, v.x, acc[0]);
-      acc[1] = fmaf(w, v.y, acc[1]);
-      acc[2] = fmaf(w, v.z, acc[2]);
-      acc[3] = fmaf(w, v.w, acc[3]);
+  const int R = tile * kBiasedTileRows + r;
+  if (R >= c.len * p.group) return;                             // all wavefronts of the row
+  if (__int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x0))) == kWhole) return;
+  const float* po = p.part_o + ((size_t)slot0 * p.parts * p.tile_rows + r) * D + DPL * lane;
+  float mx = x0;
+  for (int c0 = 64; c0 < p.parts; c0 += 64)
+    if (c0 + lane < p.parts) mx = fmaxf(mx, lse[(c0 + lane) * p.tile_rows]);
+  mx = group_max4(row_max16(mx));
+  const float mref = mx == -__builtin_inff() ? 0.f : mx;
+  float sum = 0.f, acc[DPL];
+#pragma unroll
+  for (int d = 0; d < DPL; ++d) acc[d] = 0.f;
+  for (int c0 = 0; c0 < p.parts; c0 += 64) {
+    float x = x0;
+    if (c0 > 0) x = c0 + lane < p.parts ? lse[(c0 + lane) * p.tile_rows] : -__builtin_inff();
+    // partitions that hold something come first: the others begin past the row's last token
+    const uint64_t some = __builtin_amdgcn_ballot_w64(x != -__builtin_inff());
+    if (some == 0) continue;
+    const int cnt = 64 - __builtin_clzll(some);
+    const int wl = __float_as_int(fast_exp2(x - mref));
+    for (int j0 = wave * kGroup; j0 < cnt; j0 += NW * kGroup) {
+      float v[kGroup][DPL];
+#pragma unroll
+      for (int k = 0; k < kGroup; ++k) {
+        const bool has = j0 + k < cnt && ((some >> (j0 + k)) & 1);      // uniform: its o was written
+#pragma unroll
+        for (int d = 0; d < DPL; ++d) v[k][d] = has ? po[(size_t)(c0 + j0 + k) * p.tile_rows * D + d] : 0.f;
+      }
+#pragma unroll
+      for (int k = 0; k < kGroup; ++k) {
+        const float w = j0 + k < cnt ? __int_as_float(__builtin_amdgcn_readlane(wl, j0 + k)) : 0.f;
+        sum += w;
+#pragma unroll
+        for (int d = 0; d < DPL; ++d) acc[d] = fmaf(w, v[k][d], acc[d]);
+      }
     }
-    const float inv = sum == 0.f ? 0.f : 1.0f / sum;
-    const int R = row0 + r;
-    uint16_t* dst = p.out + ((size_t)(c.start + R / p.group) * p.num_q_heads + g * p.group + R % p.group) * D + d;
-    *reinterpret_cast<uint2*>(dst) = make_uint2(bf16_rne(acc[0] * inv) | (bf16_rne(acc[1] * inv) << 16),
-                                                bf16_rne(acc[2] * inv) | (bf16_rne(acc[3] * inv) << 16));
   }
+  if constexpr (NW > 1) {
+    lds_f32_t* so = smem;                                       // [NW][D], then [NW] sums
+    lds_f32_t* sw = smem + NW * D;
+#pragma unroll
+    for (int d = 0; d < DPL; ++d) so[wave * D + DPL * lane + d] = acc[d];
+    if (lane == 0) sw[wave] = sum;
+    __syncthreads();
+    if (wave != 0) return;
+#pragma unroll
+    for (int w = 1; w < NW; ++w) {
+      sum += sw[w];
+#pragma unroll
+      for (int d = 0; d < DPL; ++d) acc[d] += so[w * D + DPL * lane + d];
+    }
+  }
+  const float inv = sum == 0.f ? 0.f : 1.0f / sum;
+  uint16_t* dst = p.out + ((size_t)(c.start + R / p.group) * p.num_q_heads + g * p.group + R % p.group) * D;
+  if constexpr (DPL == 2)
+    *reinterpret_cast<uint32_t*>(dst + 2 * lane) = bf16_rne(acc[0] * inv) | (bf16_rne(acc[1] * inv) << 16);
+  else
+    dst[lane] = (uint16_t)bf16_rne(acc[0] * inv);
 }
 
 }  // namespace biased

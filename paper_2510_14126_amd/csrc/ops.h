@@ -71,10 +71,12 @@ struct BiasedParams {
   int32_t max_chunk;
   int32_t total_q;
   int32_t window;                // 0: none
-  int32_t tiles;                 // row tiles per sequence in the grid
+  int32_t big;                   // 1: kBiasedWgRows rows per workgroup, 0: kBiasedTileRows
+  int32_t tiles;                 // row tiles (of that many rows) per sequence in the grid
   int32_t parts;                 // partitions of a tile's tokens in the grid
-  int32_t min_blocks;            // fewest blocks of a partition
+  int32_t part_blocks;           // blocks of a partition (even), where there are several
   int32_t tile_rows;             // rows of a tile that the partial buffers hold
+  int32_t stream_tiles;          // 1: load the tiles with the streaming cache hint
   float scale_log2;              // scale * log2(e)
   // softcap > 0, scores in log2 units x = raw * |scale_log2|: y = raw * (c0 + c1 raw^2
   // + c2 raw^4 + c3 raw^6) while |raw| <= raw_max, cap - 2 cap / (2^(raw * two_z) + 1) above
@@ -84,10 +86,11 @@ struct BiasedParams {
   float two_z;                   // 2 log2(e) |scale| / softcap
 };
 constexpr int kBiasedTileRows = 32;     // query rows (token x head) of a row tile
+constexpr int kBiasedWgRows = 128;      // rows of a workgroup in the form for long chunks
 
 // Rows and token partitions of a call (kernel launch and workspace size).
 struct BiasedPlan {
-  int32_t tiles, tile_rows, parts, min_blocks;
+  int32_t tiles, tile_rows, parts, part_blocks, big;
 };
 hipError_t launch_biased(const BiasedParams& p, hipStream_t stream);
 

@@ -324,9 +324,10 @@ def test_side_stream_and_two_calls_at_once():
         assert (c.out.cpu().numpy().view(np.uint16) == want).all()
 
 
-def test_captured_and_replayed():
+@pytest.mark.parametrize("window", [500, 1200])          # one partition, several
+def test_captured_and_replayed(window):
     """A step of norm, rotation, append and attention captured into a graph, replayed over changing inputs."""
-    print("[gpu case] graph", flush=True)
+    print(f"[gpu case] graph {window}", flush=True)
     hq, hkv, d, batch, steps = 16, 4, 128, 3, 6
     gen = torch.Generator(device=DEV).manual_seed(13)
     ctx = np.array([70, 1500, 31])
@@ -346,9 +347,9 @@ def test_captured_and_replayed():
                   out=torch.zeros(batch, hq, d, device=DEV, dtype=torch.bfloat16),
                   ctx=torch.tensor(ctx, dtype=torch.int32, device=DEV))
         st["pool"] = pa.kv_pool_create(blocks, 16, hkv, d, st["k"], st["v"])
-        size = pa.paged_attn_biased_workspace_size(st["pool"], batch, hq, 16 * width, 1, 500)
-        assert size > 0
-        st["ws"] = torch.zeros(size, dtype=torch.uint8, device=DEV)
+        size = pa.paged_attn_biased_workspace_size(st["pool"], batch, hq, 16 * width, 1, window)
+        assert (size > 0) == (window == 1200)
+        st["ws"] = torch.zeros(max(size, 16), dtype=torch.uint8, device=DEV)
 
         def step(stream):
             x, s = st["x"].data_ptr(), st["x"].stride(0)
@@ -356,7 +357,7 @@ def test_captured_and_replayed():
                                       x + 2 * (hq + hkv) * d, s, 1e-6, pa.PA_BF16, None, None, batch, rows, width,
                                       st["ctx"], batch, st["q"], stream)
             pa.paged_attn_decode_biased(st["pool"], st["q"], rows, width, st["ctx"], batch, hq, d ** -0.5, 30.0, None,
-                                        500, None, 16 * width, st["ws"], size, st["out"], stream)
+                                        window, None, 16 * width, st["ws"], size, st["out"], stream)
         st["step"] = step
         return st
 
