@@ -17,7 +17,7 @@ struct pa_rope {
   int32_t rotary_dim;
   int32_t layout;
   double magnitude;
-  double freqs[pa::kRopeMaxDim / 2];   // radians per position
+  double turns[pa::kRopeMaxDim / 2];   // revolutions per position
 };
 
 namespace {
@@ -60,7 +60,6 @@ int rope_params(const pa_rope* rope, int32_t num_q_heads, int32_t num_kv_heads, 
   p->rotary_dim = rope->rotary_dim;
   p->eps = eps;
   p->magnitude = (float)rope->magnitude;
-  for (int i = 0; i < rope->rotary_dim / 2; ++i) p->turns[i] = rope->freqs[i] / kTwoPi;
   return PA_OK;
 }
 
@@ -135,7 +134,7 @@ int pa_rope_create(int32_t head_dim, int32_t rotary_dim, int32_t layout, const d
   r->rotary_dim = rotary_dim;
   r->layout = layout;
   r->magnitude = magnitude;
-  for (int i = 0; i < rotary_dim / 2; ++i) r->freqs[i] = freqs[i];
+  for (int i = 0; i < rotary_dim / 2; ++i) r->turns[i] = freqs[i] / kTwoPi;
   *out = r;
   return PA_OK;
 }
@@ -173,7 +172,7 @@ int paged_attn_norm_rope(const pa_rope* rope, const void* q, int64_t q_stride, i
   p.k_out_stride = k_out_stride;
   p.positions = positions;
   p.tokens = tokens;
-  const hipError_t e = pa::launch_rope(p, dtype, rope->layout == PA_ROPE_INTERLEAVED, false,
+  const hipError_t e = pa::launch_rope(p, rope->turns, dtype, rope->layout == PA_ROPE_INTERLEAVED, false,
                                        static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return fail(PA_EHIP, "%s: kernel launch failed: %s", fn, hipGetErrorString(e));
   return PA_OK;
@@ -226,7 +225,7 @@ int paged_attn_rope_append(const pa_kv_pool* pool, const pa_rope* rope, const vo
   p.batch = batch;
   p.bt_stride = bt_stride;
   p.num_blocks = pool->num_blocks;
-  const hipError_t e = pa::launch_rope(p, dtype, rope->layout == PA_ROPE_INTERLEAVED, true,
+  const hipError_t e = pa::launch_rope(p, rope->turns, dtype, rope->layout == PA_ROPE_INTERLEAVED, true,
                                        static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return fail(PA_EHIP, "%s: kernel launch failed: %s", fn, hipGetErrorString(e));
   return PA_OK;
@@ -241,11 +240,13 @@ constexpr double kLog2e = 1.4426950408889634;
 // Rows: 128 per workgroup over one stream of its tokens (big), or 32 whose
 // tokens its wavefronts split, a chain four times shorter per workgroup: while
 // those, weighed by the tokens a chunk's average row sees against the longest
-// context, are all resident at once (two per CU), or while they are at most
-// twice the others, whose tiles are then mostly empty.  32-row / 128-row form,
-// 32 heads over 8, capped scores: one chunk of 16 over 2320 tokens 13 / 96 us,
-// of 256 over 2560 39 / 106, eight of 64 over 2368 62 / 102; three of 600 over
-// 2904 (1800 workgroups) 189 / 155, one prompt of 8191 1140 / 881.
+// context, are few, or while they are at most twice the others, whose tiles are
+// then mostly empty.  32-row / 128-row form, capped, 32 heads over 8, weighed
+// workgroups in brackets: D = 128, three chunks of 100 over 2404 tokens (306) 49 /
+// 101 us, of 300 over 2604 (859) 103 / 111, of 600 over 2904 (1610) 189 / 155, one
+// prompt of 1500 (752) 62 / 68, 2000 (1000) 98 / 91, 8191 (4096) 1140 / 881; D = 64,
+// three of 400 over 2704 (1111) 80 / 105, 500 over 2804 (1377) 92 / 114, one prompt of
+// 2000 (1000) 62 / 69, 2600 (1300) 92 / 90, 3000 (1500) 116 / 106.
 //
 // Tokens of a 32-row tile: one partition, or several, merged by a second launch
 // (2.5 us), where the tiles alone are fewer workgroups than CUs and hold more
@@ -257,14 +258,15 @@ constexpr double kLog2e = 1.4426950408889634;
 // us, 64 with a window of 4096 169 / 168 / 167, of 32 blocks 303 / 175.
 constexpr int64_t kFillWorkgroups = 256;
 constexpr int64_t kWholeBlocks = 40, kLeastBlocks = 16, kMostBlocks = 128;
-pa::BiasedPlan biased_plan(int batch, int num_kv_heads, int group, int max_ctx, int max_chunk, int window) {
+pa::BiasedPlan biased_plan(int batch, int num_kv_heads, int group, int head_dim, int max_ctx, int max_chunk, int window) {
   pa::BiasedPlan pl;
   const int64_t rows = (int64_t)std::max(max_chunk, 1) * group;
   const int64_t tiles = (rows + pa::kBiasedTileRows - 1) / pa::kBiasedTileRows;
   const int64_t big_tiles = (rows + pa::kBiasedWgRows - 1) / pa::kBiasedWgRows;
   const int64_t wgs = std::max<int64_t>(1, batch * tiles * num_kv_heads), big_wgs = batch * big_tiles * num_kv_heads;
+  const double resident = head_dim == 64 ? 1280 : 896;
   pl.big = max_chunk > 1 && wgs > 2 * big_wgs &&
-           wgs * (2.0 * max_ctx - max_chunk) > 2.0 * 2 * kFillWorkgroups * max_ctx;
+           wgs * (2.0 * max_ctx - max_chunk) > 2.0 * resident * max_ctx;
   pl.tiles = (int32_t)(pl.big ? big_tiles : tiles);
   pl.tile_rows = (int32_t)std::min<int64_t>(rows, pa::kBiasedTileRows);
   const int64_t all = ((int64_t)max_ctx + PA_BLOCK_SIZE - 1) / PA_BLOCK_SIZE;
@@ -307,7 +309,7 @@ int plan_biased(const pa_kv_pool* pool, int32_t batch, int32_t num_q_heads, int3
   *slots = (int64_t)batch * tiles;
   if (*slots > 0x7fffffffLL / pool->num_kv_heads) return fail(PA_EINVAL, "%s: grid too large", fn);
   *slots *= pool->num_kv_heads;
-  *pl = biased_plan(batch, pool->num_kv_heads, group, max_context_len, max_chunk, window);
+  *pl = biased_plan(batch, pool->num_kv_heads, group, pool->head_dim, max_context_len, max_chunk, window);
   if (*slots * pl->parts > 0x7fffffffLL) return fail(PA_EINVAL, "%s: grid too large", fn);
   return PA_OK;
 }

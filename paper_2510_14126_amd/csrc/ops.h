@@ -40,10 +40,11 @@ struct RopeParams {
   int32_t batch;
   int32_t bt_stride;
   int32_t num_blocks;
-  double turns[kRopeMaxDim / 2]; // revolutions per position of each rotated pair
 };
-// dtype: PA_BF16, PA_FP16 or PA_FP32; interleaved: pairs (2i, 2i + 1).
-hipError_t launch_rope(const RopeParams& p, int dtype, bool interleaved, bool append, hipStream_t stream);
+// turns: revolutions per position of each of the rotary_dim / 2 pairs (host
+// memory); dtype: PA_BF16, PA_FP16 or PA_FP32; interleaved: pairs (2i, 2i + 1).
+hipError_t launch_rope(const RopeParams& p, const double* turns, int dtype, bool interleaved, bool append,
+                       hipStream_t stream);
 
 // Attention of new tokens over their sequences' paged context with capped,
 // biased or masked scores.

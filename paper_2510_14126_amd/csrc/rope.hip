@@ -33,7 +33,15 @@ namespace pa {
 namespace {
 
 constexpr int kWaves = 4;
-constexpr int kMaxPairs = kRopeMaxDim / 2;
+
+// The revolutions travel with the kernel's arguments, as many as LP lanes per
+// row have pairs: the library owns no device memory, and a launch takes the host
+// longer the more bytes of arguments it has (four tokens at D = 64, whole call: a
+// fixed array of 128 pairs 5.1 us, these 32 4.8 us).
+template <int PAIRS>
+struct Turns {
+  double of[PAIRS];
+};
 
 typedef __attribute__((address_space(3))) mfma::floatx4_t lds_f4_t;
 
@@ -135,8 +143,9 @@ __device__ __forceinline__ int sequence_of(const int32_t* q_start, int batch, in
 }
 
 template <typename T, int LP, bool INTERLEAVED, bool APPEND>
-__global__ void __launch_bounds__(64 * kWaves) rope_kernel(const RopeParams p) {
+__global__ void __launch_bounds__(64 * kWaves) rope_kernel(const RopeParams p, const Turns<8 * LP> turns) {
   using Out = std::conditional_t<APPEND, Bf16, T>;
+  constexpr int kMaxPairs = 8 * LP;
   __shared__ __attribute__((aligned(16))) float angles[kWaves][2][kMaxPairs];
   constexpr int kRows = 64 / LP;                  // rows of one step
   const int lane = threadIdx.x & 63;
@@ -211,7 +220,7 @@ __global__ void __launch_bounds__(64 * kWaves) rope_kernel(const RopeParams p) {
   {
     lds_f32_t* mine = (lds_f32_t*)&angles[wave][0][0];
     for (int i = lane; i < p.rotary_dim / 2; i += 64) {
-      const double turn = (double)pos * p.turns[i];
+      const double turn = (double)pos * turns.of[i];
       float s, co;
       sincospif(2.0f * (float)(turn - rint(turn)), &s, &co);
       mine[i] = co * p.magnitude;
@@ -309,16 +318,26 @@ __global__ void __launch_bounds__(64 * kWaves) rope_kernel(const RopeParams p) {
 }
 
 template <typename T, int LP>
-hipError_t launch_t(RopeParams p, bool interleaved, bool append, hipStream_t stream) {
+hipError_t launch_t(RopeParams p, const double* host_turns, bool interleaved, bool append, hipStream_t stream) {
   const int total = p.num_q_heads + (append ? 2 : 1) * p.num_kv_heads;
   const int steps = (total * LP + 63) / 64;
-  // Wavefronts per token: enough to fill the GPU while tokens are few, then one
-  // for all rows of a token, whose angles it computes once.
-  constexpr int64_t kFill = 8192;
-  p.waves = (int)std::max<int64_t>(1, std::min<int64_t>(steps, kFill / p.tokens));
+  // Steps of one wavefront: one while tokens are few; more once the call fills
+  // the GPU several times over, which saves angles and launches, but leaves an
+  // uneven end if there are too few wavefronts.  Normed, rotated, D = 128, at
+  // 16384 / 32768 / 65536 / 131072 / 262144 / 10^6 steps in flight: 8191 tokens of 72
+  // rows 62.0 / 59.7 / 59.0 / 61.8 / 61.8 / 61.7 us (5.1 TB/s at best, a copy of the same
+  // bytes reaches 5.2-5.4), append of 53.6K tokens of 48 rows 247.8 / 247.9 / 240.8 / 241.6 /
+  // 238.8 / 285.3 us (5.5 TB/s).  Loads with the streaming hint: 57.9 and 257 us.
+  constexpr int64_t kFill = 65536;
+  const int64_t per_wave = std::min<int64_t>(steps, ((int64_t)steps * p.tokens + kFill - 1) / kFill);
+  p.waves = (int)((steps + per_wave - 1) / per_wave);
   const int64_t grid = ((int64_t)p.tokens * p.waves + kWaves - 1) / kWaves;
   if (grid > 0x7fffffffLL) return hipErrorInvalidValue;
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * kWaves), 0, stream, p); };
+  Turns<8 * LP> turns{};
+  std::copy(host_turns, host_turns + p.rotary_dim / 2, turns.of);
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(64 * kWaves), 0, stream, p, turns);
+  };
   if (append)
     interleaved ? go(rope_kernel<T, LP, true, true>) : go(rope_kernel<T, LP, false, true>);
   else
@@ -327,18 +346,19 @@ hipError_t launch_t(RopeParams p, bool interleaved, bool append, hipStream_t str
 }
 
 template <typename T>
-hipError_t launch_d(const RopeParams& p, bool interleaved, bool append, hipStream_t stream) {
-  if (p.head_dim <= 64) return launch_t<T, 4>(p, interleaved, append, stream);
-  if (p.head_dim <= 128) return launch_t<T, 8>(p, interleaved, append, stream);
-  return launch_t<T, 16>(p, interleaved, append, stream);
+hipError_t launch_d(const RopeParams& p, const double* turns, bool interleaved, bool append, hipStream_t stream) {
+  if (p.head_dim <= 64) return launch_t<T, 4>(p, turns, interleaved, append, stream);
+  if (p.head_dim <= 128) return launch_t<T, 8>(p, turns, interleaved, append, stream);
+  return launch_t<T, 16>(p, turns, interleaved, append, stream);
 }
 
 }  // namespace
 
-hipError_t launch_rope(const RopeParams& p, int dtype, bool interleaved, bool append, hipStream_t stream) {
-  if (dtype == PA_BF16) return launch_d<Bf16>(p, interleaved, append, stream);
-  if (dtype == PA_FP16) return launch_d<Fp16>(p, interleaved, append, stream);
-  return launch_d<Fp32>(p, interleaved, append, stream);
+hipError_t launch_rope(const RopeParams& p, const double* turns, int dtype, bool interleaved, bool append,
+                       hipStream_t stream) {
+  if (dtype == PA_BF16) return launch_d<Bf16>(p, turns, interleaved, append, stream);
+  if (dtype == PA_FP16) return launch_d<Fp16>(p, turns, interleaved, append, stream);
+  return launch_d<Fp32>(p, turns, interleaved, append, stream);
 }
 
 }  // namespace pa

@@ -3,6 +3,6 @@
 #include "ops.h"
 
 namespace pa {
-hipError_t launch_rope(const RopeParams&, int, bool, bool, hipStream_t) { return hipErrorNotSupported; }
+hipError_t launch_rope(const RopeParams&, const double*, int, bool, bool, hipStream_t) { return hipErrorNotSupported; }
 hipError_t launch_biased(const BiasedParams&, hipStream_t) { return hipErrorNotSupported; }
 }  // namespace pa
