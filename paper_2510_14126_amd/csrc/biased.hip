@@ -29,9 +29,10 @@ biased_decode_kernel(const BiasedParams p) {
   biased::decode_body<D, GP, CAP, BIAS, AUX>(p, blockIdx.x, (lds_u8_t*)smem);
 }
 
-// One row per workgroup (NW = 4 wavefronts on it), or four (NW = 1).
+// One row per workgroup, NW = 8 wavefronts on it, or four rows (NW = 1).
+constexpr int kMergeWaves = 8;
 template <int D, int NW>
-__global__ void __launch_bounds__(64 * kWaves) biased_merge_kernel(const BiasedParams p) {
+__global__ void __launch_bounds__(64 * (NW > 1 ? NW : kWaves)) biased_merge_kernel(const BiasedParams p) {
   __shared__ __attribute__((aligned(16))) float smem[NW > 1 ? NW * (D + 1) : 1];
   const int wave = wave_uniform(threadIdx.x >> 6);
   const int64_t row = NW > 1 ? blockIdx.x : (int64_t)blockIdx.x * kWaves + wave;
@@ -60,7 +61,8 @@ hipError_t launch_t(const BiasedParams& p, hipStream_t stream) {
   if (p.parts > 1) {
     const int64_t rows = tiles * p.tile_rows;
     if (p.parts > biased::kGroup && rows <= 512)
-      hipLaunchKernelGGL((biased_merge_kernel<D, kWaves>), dim3((unsigned)rows), dim3(64 * kWaves), 0, stream, p);
+      hipLaunchKernelGGL((biased_merge_kernel<D, kMergeWaves>), dim3((unsigned)rows), dim3(64 * kMergeWaves), 0, stream,
+                         p);
     else
       hipLaunchKernelGGL((biased_merge_kernel<D, 1>), dim3((unsigned)((rows + kWaves - 1) / kWaves)), dim3(64 * kWaves),
                          0, stream, p);

@@ -134,17 +134,15 @@ __device__ __forceinline__ Row row_of(const BiasedParams& p, const Chunk& c, int
   return r;
 }
 
-// A raw score capped, in log2 units; far: some score of the stage is beyond the
-// polynomial (wave-uniform).
-__device__ __forceinline__ float cap_score(const BiasedParams& p, float x, bool far) {
+// A raw score capped, in log2 units: within the polynomial's range, and anywhere.
+__device__ __forceinline__ float cap_near(const BiasedParams& p, float x) {
   const float u = x * x;
-  float y = x * fmaf(u, fmaf(u, fmaf(u, p.c3, p.c2), p.c1), p.c0);
-  if (far) {
-    const float t = fast_exp2(x * p.two_z);
-    const float z = fmaf(-2.f * p.cap, __builtin_amdgcn_rcpf(t + 1.f), p.cap);
-    y = fabsf(x) <= p.raw_max ? y : z;
-  }
-  return y;
+  return x * fmaf(u, fmaf(u, fmaf(u, p.c3, p.c2), p.c1), p.c0);
+}
+__device__ __forceinline__ float cap_any(const BiasedParams& p, float x) {
+  const float t = fast_exp2(x * p.two_z);
+  const float z = fmaf(-2.f * p.cap, __builtin_amdgcn_rcpf(t + 1.f), p.cap);
+  return fabsf(x) <= p.raw_max ? cap_near(p, x) : z;
 }
 
 // The 32 columns of one wavefront: queries (Q^T operand of step s: dims 16s + 8h
@@ -155,6 +153,7 @@ struct Columns {
   float m, neg, l;              // running max, -m (0 while it is -inf), the lane's share of the sum
   floatx16_t o[D / 32];         // [j][r]: row 8(r/4) + 4h + r%4, dim 32j + n
   float scale;                  // |scale_log2|
+  float base;                   // of the shaped stage (see shape)
 
   // Operand of step s from the row's memory; bf16 negation is exact.
   static __device__ __forceinline__ u32x4_t query(const BiasedParams& p, const uint16_t* q_row, int s, int h) {
@@ -191,23 +190,41 @@ struct Columns {
     return a;
   }
 
-  // Cap, bias and masks of a stage whose first token is t0.  With CAP or BIAS
-  // the scores become log2 units; else they stay raw.
-  __device__ __forceinline__ void shape(const BiasedParams& p, floatx16_t& a, int t0, bool edge, int h) const {
+  // Cap, bias and masks of a stage whose first token is t0; `linear`: no row's
+  // position is before the stage's last token.  Without CAP and BIAS the scores
+  // stay raw; with CAP alone they become log2 units; so with BIAS, in a linear
+  // stage without the part of the bias that all its tokens share, base = slope
+  // (t0 + 4h - p): one FMA per score adds slope (t - t0 - 4h), and base goes where
+  // the running max does.
+  __device__ __forceinline__ void shape(const BiasedParams& p, floatx16_t& a, int t0, bool edge, bool linear, int h) {
     if constexpr (CAP) {
       float most = 0.f;
 #pragma unroll
       for (int r = 0; r < 16; ++r) most = fmaxf(most, fabsf(a[r]));
-      const bool far = __builtin_amdgcn_ballot_w64(!(most <= p.raw_max)) != 0;
+      if (__builtin_amdgcn_ballot_w64(!(most <= p.raw_max)) != 0) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) a[r] = cap_score(p, a[r], far);
+        for (int r = 0; r < 16; ++r) a[r] = cap_any(p, a[r]);
+      } else {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) a[r] = cap_near(p, a[r]);
+      }
     }
+    base = 0.f;
     if constexpr (BIAS) {
       const float d0 = row.pos - (float)(t0 + 4 * h);
+      if (linear) {
+        base = -row.slope * d0;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float y = CAP ? a[r] : a[r] * scale;
-        a[r] = fmaf(-row.slope, fabsf(d0 - (float)(8 * (r >> 2) + (r & 3))), y);
+        for (int r = 0; r < 16; ++r) {
+          const float off = row.slope * (float)(8 * (r >> 2) + (r & 3));
+          a[r] = CAP ? a[r] + off : fmaf(a[r], scale, off);
+        }
+      } else {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const float y = CAP ? a[r] : a[r] * scale;
+          a[r] = fmaf(-row.slope, fabsf(d0 - (float)(8 * (r >> 2) + (r & 3))), y);
+        }
       }
     }
     if (edge) {
@@ -217,10 +234,6 @@ struct Columns {
       for (int r = 0; r < 16; ++r)
         if ((unsigned)(from + 8 * (r >> 2) + (r & 3)) >= span) a[r] = -__builtin_inff();
     }
-  }
-
-  __device__ __forceinline__ float weight(float a) const {
-    return fast_exp2(CAP || BIAS ? a + neg : fmaf(a, scale, neg));
   }
 
   // One value per row, from the lane (h, n) that holds it as column n to the
@@ -243,7 +256,10 @@ struct Columns {
     float x = a[0];
 #pragma unroll
     for (int r = 1; r < 16; ++r) x = fmaxf(x, a[r]);
-    if (!(CAP || BIAS)) x *= scale;
+    if constexpr (BIAS)
+      x += base;
+    else if constexpr (!CAP)
+      x *= scale;
     if (__builtin_amdgcn_ballot_w64(x > m + kLazyRescale) != 0) {
       float y = x;
       swap32(x, y);
@@ -267,16 +283,19 @@ struct Columns {
 
   // Weights of the shaped scores a and their PV with the stage at st.
   __device__ __forceinline__ void attend(const floatx16_t& a, const lds_u8_t* st, int lane) {
+    float w[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) w[r] = fast_exp2(CAP || BIAS ? a[r] + (BIAS ? neg + base : neg) : fmaf(a[r], scale, neg));
     u32x4_t hi[2], lo[2];
     float sum[2];
 #pragma unroll
     for (int mb = 0; mb < 2; ++mb)
 #pragma unroll
       for (int e = 0; e < 8; e += 2) {
-        const float p0 = weight(a[8 * mb + e]), p1 = weight(a[8 * mb + e + 1]);
-        const uint32_t w = pack_bf16(p0, p1);
-        hi[mb][e / 2] = w;
-        lo[mb][e / 2] = pack_bf16(p0 - bf16_lo(w), p1 - bf16_hi(w));
+        const float p0 = w[8 * mb + e], p1 = w[8 * mb + e + 1];
+        const uint32_t x = pack_bf16(p0, p1);
+        hi[mb][e / 2] = x;
+        lo[mb][e / 2] = pack_bf16(p0 - bf16_lo(x), p1 - bf16_hi(x));
         sum[mb] = e == 0 ? p0 + p1 : sum[mb] + (p0 + p1);
       }
     l += sum[0] + sum[1];
@@ -328,6 +347,22 @@ struct Columns {
       }
     }
   }
+};
+
+// The order of a range's stages: with a distance bias from the nearest tokens to
+// the farthest, so that the running max is found first (upwards it rises with
+// every stage of a steep head, and each rise rescales the outputs: a prompt of
+// 8191 tokens 860 us, downwards DOWN).  at(s): stage of step s (past the last step
+// the last stage again); chunk(s): which 64 blocks hold it.
+template <bool DOWN>
+struct Walk {
+  int n;
+  static constexpr int kStep = DOWN ? -1 : 1;
+  __device__ __forceinline__ int at(int s) const {
+    const int t = max(min(s, n - 1), 0);
+    return DOWN ? max(n - 1, 0) - t : t;
+  }
+  __device__ __forceinline__ int chunk(int s) const { return 2 * at(s) >> 6; }
 };
 
 // A packed pair of bf16 with zeros for infinities and NaN; marks them in `odd`.
@@ -418,6 +453,12 @@ __device__ __forceinline__ void split_body(const BiasedParams& p, int wg, lds_u8
 
   // A column without a row repeats the tile's first and is not written.
   const int R = row0 + n < rows ? row0 + n : row0;
+  u32x4_t q_mine[D / 64];                              // this wavefront's share of the queries
+  {
+    const uint16_t* q_row = p.q + ((size_t)(c.start + R / p.group) * p.num_q_heads + g * p.group + R % p.group) * D;
+#pragma unroll
+    for (int i = 0; i < D / 64; ++i) q_mine[i] = Columns<D, CAP, BIAS>::query(p, q_row, wave * (D / 64) + i, h);
+  }
   const Row row = row_of<BIAS>(p, c, b, g, R);
   const bool none = row.hi <= row.lo;
   const int lo = min32(none ? 0x3fffffff : row.lo);     // tokens that some row sees
@@ -425,6 +466,7 @@ __device__ __forceinline__ void split_body(const BiasedParams& p, int wg, lds_u8
   const int all_lo = max32(row.lo);                     // tokens that every row sees
   const int all_hi = min32(none ? 0 : row.hi);
 
+  const int from_pos = c.first + row0 / p.group;        // position of the tile's first row
   // This partition's blocks.
   const int first = lo >> 4;
   const int nblk = hi > lo ? ((hi + 15) >> 4) - first : 0;
@@ -443,14 +485,8 @@ __device__ __forceinline__ void split_body(const BiasedParams& p, int wg, lds_u8
   // The queries stay in LDS (all wavefronts have the same rows): in registers
   // they would not fit beside a stage in flight.
   lds_u32x4_t* ql = reinterpret_cast<lds_u32x4_t*>(smem + kSplitQuery<D>) + lane;
-  {
-    const uint16_t* q_row = p.q + ((size_t)(c.start + R / p.group) * p.num_q_heads + g * p.group + R % p.group) * D;
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i) {
-      const int s = wave * (D / 64) + i;
-      ql[64 * s] = C.query(p, q_row, s, h);
-    }
-  }
+  for (int i = 0; i < D / 64; ++i) ql[64 * (wave * (D / 64) + i)] = q_mine[i];
 
   constexpr size_t kTile = 16 * D;
   const size_t blk_stride = (size_t)p.num_kv_heads * kTile;
@@ -470,21 +506,25 @@ __device__ __forceinline__ void split_body(const BiasedParams& p, int wg, lds_u8
   // Block ids, one per lane: those of the 64 blocks being loaded and the next 64.
   auto ids_of = [&](int chunk) {
     const int j = 64 * chunk + lane;
-    return j < cnt ? min(max(bt[j], 0), p.num_blocks - 1) : 0;
+    return j >= 0 && j < cnt ? min(max(bt[j], 0), p.num_blocks - 1) : 0;
   };
-  int ids = whole ? (lane < cnt ? min(max(ids_first, 0), p.num_blocks - 1) : 0) : ids_of(0);
-  int ids_next = ids_of(1), chunk = 0;
+  const Walk<BIAS> walk{nstage};
+  int chunk = walk.chunk(wave);
+  int ids = whole && chunk == 0 ? (lane < cnt ? min(max(ids_first, 0), p.num_blocks - 1) : 0) : ids_of(chunk);
+  int ids_next = ids_of(chunk + walk.kStep);
   auto load = [&](int s) {
-    if (2 * s >> 6 != chunk) {                            // uniform; a wavefront's stages skip no chunk
+    if (walk.chunk(s) != chunk) {                         // uniform; a wavefront's stages skip no chunk
       ids = ids_next;
-      ids_next = ids_of(++chunk + 1);
+      chunk += walk.kStep;
+      ids_next = ids_of(chunk + walk.kStep);
     }
+    const int j = 2 * walk.at(s);
     int id[2];
 #pragma unroll
-    for (int e = 0; e < 2; ++e) id[e] = __builtin_amdgcn_readlane(ids, (2 * s + e) & 63);
+    for (int e = 0; e < 2; ++e) id[e] = __builtin_amdgcn_readlane(ids, (j + e) & 63);
 #pragma unroll
     for (int e = 0; e < 2; ++e) {
-      const int bytes = 2 * s + e < cnt ? (int)kTile * 2 : 0;      // none past the last block: zeros
+      const int bytes = s < nstage && j + e < cnt ? (int)kTile * 2 : 0;      // none past the last block: zeros
       const __amdgpu_buffer_rsrc_t dk = __builtin_amdgcn_make_buffer_rsrc(
           const_cast<uint16_t*>(kbase + (size_t)id[e] * blk_stride), 0, bytes, kBufferDescWord3);
       const __amdgpu_buffer_rsrc_t dv = __builtin_amdgcn_make_buffer_rsrc(
@@ -506,12 +546,13 @@ __device__ __forceinline__ void split_body(const BiasedParams& p, int wg, lds_u8
   load(wave);
   __syncthreads();
   for (int s = wave; s < nstage; s += kWaves) {
-    const int t0 = (j0 + 2 * s) * 16;
+    const int t0 = (j0 + 2 * walk.at(s)) * 16;
     const bool edge = t0 < all_lo || t0 + kTokens > all_hi;       // uniform
     if (edge) {
+      const int t_lane = t0 + lrow;
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
-        const int t = t0 + i * kRowsPerLoad + lrow;
+        const int t = t_lane + i * kRowsPerLoad;
         if (t < lo || t >= hi) {
           rk[i] = u32x4_t{0, 0, 0, 0};
           rv[i] = u32x4_t{0, 0, 0, 0};
@@ -528,7 +569,7 @@ __device__ __forceinline__ void split_body(const BiasedParams& p, int wg, lds_u8
     }
     load(s + kWaves);
     floatx16_t a = C.scores(st, h, n, [&](int i) { return ql[64 * i]; });
-    C.shape(p, a, t0, edge, h);
+    C.shape(p, a, t0, edge, t0 + kTokens <= from_pos + 1, h);
     C.raise(a, rowv, h, n);
     C.attend(a, st, lane);
   }
@@ -596,7 +637,11 @@ __device__ __forceinline__ void split_body(const BiasedParams& p, int wg, lds_u8
           } else {
             uint16_t* dst = p.out + ((size_t)(c.start + Rr / p.group) * p.num_q_heads + g * p.group + Rr % p.group) * D;
 #pragma unroll
-            for (int j = 0; j < kJ; ++j) dst[32 * j + n] = (uint16_t)bf16_rne(acc[j]);
+            for (int j = 0; j < kJ; j += 2) {
+              const uint32_t x = pack_bf16(acc[j], acc[j + 1]);
+              dst[32 * j + n] = (uint16_t)x;
+              dst[32 * j + 32 + n] = (uint16_t)(x >> 16);
+            }
           }
         }
       }
@@ -638,6 +683,12 @@ __device__ __forceinline__ void big_body(const BiasedParams& p, int wg, lds_u8_t
 
   // A column without a row repeats the workgroup's first and is not written.
   const int R = row0 + n < rows ? row0 + n : tile * kBiasedWgRows;
+  u32x4_t q[D / 16];
+  {
+    const uint16_t* q_row = p.q + ((size_t)(c.start + R / p.group) * p.num_q_heads + g * p.group + R % p.group) * D;
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) q[s] = Columns<D, CAP, BIAS>::query(p, q_row, s, h);
+  }
   const Row row = row_of<BIAS>(p, c, b, g, R);
   int lo, hi, all_lo, all_hi;                          // tokens that some row, that every row of the workgroup sees
   {
@@ -661,17 +712,12 @@ __device__ __forceinline__ void big_body(const BiasedParams& p, int wg, lds_u8_t
     all_hi = -y[3];
     __syncthreads();                                   // `range` is used again
   }
+  const int from_pos = c.first + tile * kBiasedWgRows / p.group;   // position of the workgroup's first row
   const int j0 = lo >> 4;
   const int cnt = hi > lo ? ((hi + 15) >> 4) - j0 : 0;
 
   Columns<D, CAP, BIAS> C;
   C.init(p, row);
-  u32x4_t q[D / 16];
-  {
-    const uint16_t* q_row = p.q + ((size_t)(c.start + R / p.group) * p.num_q_heads + g * p.group + R % p.group) * D;
-#pragma unroll
-    for (int s = 0; s < D / 16; ++s) q[s] = C.query(p, q_row, s, h);
-  }
   auto query = [&](int s) { return q[s]; };
 
   constexpr size_t kTile = 16 * D;
@@ -679,11 +725,14 @@ __device__ __forceinline__ void big_body(const BiasedParams& p, int wg, lds_u8_t
   const uint16_t* kbase = p.k_pool + (size_t)g * kTile;
   const uint16_t* vbase = p.v_pool + (size_t)g * kTile;
   const int32_t* bt = p.block_tables + (size_t)b * p.bt_stride + j0;
+  const int nstage = (cnt + 1) >> 1;
   auto ids_of = [&](int chunk) {
     const int j = 64 * chunk + lane;
-    return j < cnt ? min(max(bt[j], 0), p.num_blocks - 1) : 0;
+    return j >= 0 && j < cnt ? min(max(bt[j], 0), p.num_blocks - 1) : 0;
   };
-  int ids = ids_of(0), ids_next = ids_of(1), chunk = 0;
+  const Walk<BIAS> walk{nstage};
+  int chunk = walk.chunk(0);
+  int ids = ids_of(chunk), ids_next = ids_of(chunk + walk.kStep);
 
   // The workgroup's share of a stage: 256 threads take 16 bytes each of K and V,
   // D / 64 times: whole blocks (D = 128) or both halves at once (D = 64).
@@ -693,15 +742,16 @@ __device__ __forceinline__ void big_body(const BiasedParams& p, int wg, lds_u8_t
   const int lane_off = (D == 128 ? threadIdx.x : threadIdx.x & 127) * 16;
   u32x4_t rk[kLoads], rv[kLoads];
   auto load = [&](int s) {
-    if (2 * s >> 6 != chunk) {                         // uniform
+    if (walk.chunk(s) != chunk) {                      // uniform
       ids = ids_next;
-      ids_next = ids_of(++chunk + 1);
+      chunk += walk.kStep;
+      ids_next = ids_of(chunk + walk.kStep);
     }
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const int j = 2 * s + (D == 128 ? i : wave >> 1);
+      const int j = 2 * walk.at(s) + (D == 128 ? i : wave >> 1);
       const size_t id = (size_t)__builtin_amdgcn_readlane(ids, j & 63);
-      const int bytes = j < cnt ? (int)kTile * 2 : 0;  // none past the last block: zeros
+      const int bytes = s < nstage && j < cnt ? (int)kTile * 2 : 0;  // none past the last block: zeros
       const __amdgpu_buffer_rsrc_t dk = __builtin_amdgcn_make_buffer_rsrc(
           const_cast<uint16_t*>(kbase + id * blk_stride), 0, bytes, kBufferDescWord3);
       const __amdgpu_buffer_rsrc_t dv = __builtin_amdgcn_make_buffer_rsrc(
@@ -710,14 +760,15 @@ __device__ __forceinline__ void big_body(const BiasedParams& p, int wg, lds_u8_t
       rv[i] = __builtin_bit_cast(u32x4_t, __builtin_amdgcn_raw_buffer_load_b128(dv, lane_off, 0, 0));
     }
   };
-  auto first_of = [&](int s) { return (j0 + 2 * s) * 16; };
+  auto first_of = [&](int s) { return (j0 + 2 * walk.at(s)) * 16; };
   auto edge = [&](int s) { return first_of(s) < all_lo || first_of(s) + kTokens > all_hi; };
   uint32_t odd = 0;                                    // infinities or NaN among V where there are masks
   auto publish = [&](int s, int slot) {
     if (edge(s)) {
+      const int t_lane = first_of(s) + lrow;
 #pragma unroll
       for (int i = 0; i < kLoads; ++i) {
-        const int t = first_of(s) + 16 * i + lrow;
+        const int t = t_lane + 16 * i;
         if (t < lo || t >= hi) {
           rk[i] = u32x4_t{0, 0, 0, 0};
           rv[i] = u32x4_t{0, 0, 0, 0};
@@ -735,7 +786,6 @@ __device__ __forceinline__ void big_body(const BiasedParams& p, int wg, lds_u8_t
   };
   lds_f32_t* rowv = reinterpret_cast<lds_f32_t*>(smem + kBigRow<D>) + wave * kBiasedTileRows;
 
-  const int nstage = (cnt + 1) >> 1;
   load(0);
   publish(0, 0);
   load(1);
@@ -743,7 +793,7 @@ __device__ __forceinline__ void big_body(const BiasedParams& p, int wg, lds_u8_t
   load(2);
   __syncthreads();
   floatx16_t a = C.scores(smem, h, n, query);
-  C.shape(p, a, first_of(0), edge(0), h);
+  C.shape(p, a, first_of(0), edge(0), first_of(0) + kTokens <= from_pos + 1, h);
   C.raise(a, rowv, h, n);
   for (int s0 = 0; s0 < nstage; s0 += kSlots) {
 #pragma unroll
@@ -755,7 +805,7 @@ __device__ __forceinline__ void big_body(const BiasedParams& p, int wg, lds_u8_t
         load(s + 3);
         C.attend(a, smem + u * kStageBytes<D>, lane);
         if (s + 1 < nstage) {
-          C.shape(p, next, first_of(s + 1), edge(s + 1), h);
+          C.shape(p, next, first_of(s + 1), edge(s + 1), first_of(s + 1) + kTokens <= from_pos + 1, h);
           C.raise(next, rowv, h, n);
         }
         a = next;
@@ -784,9 +834,12 @@ __device__ __forceinline__ void big_body(const BiasedParams& p, int wg, lds_u8_t
 #pragma unroll
   for (int r = 0; r < 16; ++r)
 #pragma unroll
-    for (int j = 0; j < D / 32; ++j)
-      *reinterpret_cast<lds_u16_t*>(out + (8 * (r >> 2) + 4 * h + (r & 3)) * (D * 2) + (32 * j + n) * 2) =
-          (uint16_t)bf16_rne(C.o[j][r] * inv[r]);
+    for (int j = 0; j < D / 32; j += 2) {
+      const uint32_t x = pack_bf16(C.o[j][r] * inv[r], C.o[j + 1][r] * inv[r]);
+      lds_u16_t* dst = reinterpret_cast<lds_u16_t*>(out + (8 * (r >> 2) + 4 * h + (r & 3)) * (D * 2) + (32 * j + n) * 2);
+      dst[0] = (uint16_t)x;
+      dst[32] = (uint16_t)(x >> 16);
+    }
   __builtin_amdgcn_wave_barrier();
   constexpr int kRowsPerStore = 64 / kChunks;
 #pragma unroll
@@ -816,11 +869,23 @@ __device__ __forceinline__ void merge_body(const BiasedParams& p, int slot0, int
   const int b = wg / p.tiles;
   const float* lse = p.part_lse + (size_t)slot0 * p.parts * p.tile_rows + r;
   const float x0 = lane < p.parts ? lse[lane * p.tile_rows] : -__builtin_inff();
+  const float* po = p.part_o + ((size_t)slot0 * p.parts * p.tile_rows + r) * D + DPL * lane;
+  // Where rows are few (NW > 1) the first group is loaded before lse tells which
+  // partitions hold something; what the others' slots hold is not used.
+  float v[kGroup][DPL];
+  auto load_group = [&](int first, uint64_t some) {
+#pragma unroll
+    for (int k = 0; k < kGroup; ++k) {
+      const bool has = (some >> k) & 1;                           // uniform
+#pragma unroll
+      for (int d = 0; d < DPL; ++d) v[k][d] = has ? po[(size_t)(first + k) * p.tile_rows * D + d] : 0.f;
+    }
+  };
+  if constexpr (NW > 1) load_group(wave * kGroup, p.parts > wave * kGroup ? ~0ull >> (64 - min(p.parts - wave * kGroup, 64)) : 0);
   const Chunk c = chunk_of(p, b);
   const int R = tile * kBiasedTileRows + r;
   if (R >= c.len * p.group) return;                             // all wavefronts of the row
   if (__int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x0))) == kWhole) return;
-  const float* po = p.part_o + ((size_t)slot0 * p.parts * p.tile_rows + r) * D + DPL * lane;
   float mx = x0;
   for (int c0 = 64; c0 < p.parts; c0 += 64)
     if (c0 + lane < p.parts) mx = fmaxf(mx, lse[(c0 + lane) * p.tile_rows]);
@@ -838,16 +903,12 @@ __device__ __forceinline__ void merge_body(const BiasedParams& p, int slot0, int
     const int cnt = 64 - __builtin_clzll(some);
     const int wl = __float_as_int(fast_exp2(x - mref));
     for (int j0 = wave * kGroup; j0 < cnt; j0 += NW * kGroup) {
-      float v[kGroup][DPL];
+      const uint64_t here = some >> j0;
+      if (NW == 1 || c0 + j0 > wave * kGroup) load_group(c0 + j0, here);
 #pragma unroll
       for (int k = 0; k < kGroup; ++k) {
-        const bool has = j0 + k < cnt && ((some >> (j0 + k)) & 1);      // uniform: its o was written
-#pragma unroll
-        for (int d = 0; d < DPL; ++d) v[k][d] = has ? po[(size_t)(c0 + j0 + k) * p.tile_rows * D + d] : 0.f;
-      }
-#pragma unroll
-      for (int k = 0; k < kGroup; ++k) {
-        const float w = j0 + k < cnt ? __int_as_float(__builtin_amdgcn_readlane(wl, j0 + k)) : 0.f;
+        if (!((here >> k) & 1)) continue;
+        const float w = __int_as_float(__builtin_amdgcn_readlane(wl, j0 + k));
         sum += w;
 #pragma unroll
         for (int d = 0; d < DPL; ++d) acc[d] = fmaf(w, v[k][d], acc[d]);
@@ -872,9 +933,9 @@ __device__ __forceinline__ void merge_body(const BiasedParams& p, int slot0, int
   const float inv = sum == 0.f ? 0.f : 1.0f / sum;
   uint16_t* dst = p.out + ((size_t)(c.start + R / p.group) * p.num_q_heads + g * p.group + R % p.group) * D;
   if constexpr (DPL == 2)
-    *reinterpret_cast<uint32_t*>(dst + 2 * lane) = bf16_rne(acc[0] * inv) | (bf16_rne(acc[1] * inv) << 16);
+    *reinterpret_cast<uint32_t*>(dst + 2 * lane) = pack_bf16(acc[0] * inv, acc[1] * inv);
   else
-    dst[lane] = (uint16_t)bf16_rne(acc[0] * inv);
+    dst[lane] = (uint16_t)pack_bf16(acc[0] * inv, 0.f);
 }
 
 }  // namespace biased

@@ -79,8 +79,13 @@ __device__ __forceinline__ void decode_tile(const BiasedParams& p, WaveState<D>&
   if constexpr (CAP) {
     const float most = fmaxf(fmaxf(fabsf(raw[0]), fabsf(raw[1])), fmaxf(fabsf(raw[2]), fabsf(raw[3])));
     const bool far = __builtin_amdgcn_ballot_w64(!(most <= p.raw_max)) != 0;
+    if (far) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) e[r] = cap_score(p, raw[r], far);
+      for (int r = 0; r < 4; ++r) e[r] = cap_any(p, raw[r]);
+    } else {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) e[r] = cap_near(p, raw[r]);
+    }
   } else {
 #pragma unroll
     for (int r = 0; r < 4; ++r) e[r] = raw[r] * scale;
@@ -91,9 +96,10 @@ __device__ __forceinline__ void decode_tile(const BiasedParams& p, WaveState<D>&
     for (int r = 0; r < 4; ++r) e[r] = fmaf(-slope, fabsf(d0 - (float)(4 * r)), e[r]);
   }
   if (edge) {
+    const int t_lane = t0 + q;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int t = t0 + 4 * r + q;
+      const int t = t_lane + 4 * r;
       const bool seen = t >= lo && t < hi;
       e[r] = seen ? e[r] : -__builtin_inff();
 #pragma unroll
@@ -307,7 +313,7 @@ __device__ __forceinline__ void decode_body(const BiasedParams& p, int wg, lds_u
       if (d == 0) p.part_lse[slot * p.tile_rows + r] = lt == 0.f ? -__builtin_inff() : mref + log2f(lt);
     } else {
       const size_t row = (size_t)b * p.num_q_heads + head0 + r;
-      *reinterpret_cast<uint32_t*>(p.out + row * D + d) = bf16_rne(o0 * inv) | (bf16_rne(o1 * inv) << 16);
+      *reinterpret_cast<uint32_t*>(p.out + row * D + d) = pack_bf16(o0 * inv, o1 * inv);
       if (d == 0 && p.parts > 1) p.part_lse[slot * p.tile_rows + r] = kWhole;
     }
   }
