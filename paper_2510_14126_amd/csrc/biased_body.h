@@ -352,7 +352,7 @@ struct Columns {
 // The order of a range's stages: with a distance bias from the nearest tokens to
 // the farthest, so that the running max is found first (upwards it rises with
 // every stage of a steep head, and each rise rescales the outputs: a prompt of
-// 8191 tokens 860 us, downwards DOWN).  at(s): stage of step s (past the last step
+// 8191 tokens upwards 881 us, downwards 779).  at(s): stage of step s (past the last step
 // the last stage again); chunk(s): which 64 blocks hold it.
 template <bool DOWN>
 struct Walk {
@@ -372,17 +372,18 @@ __device__ __forceinline__ uint32_t finite_part(uint32_t x, uint32_t& odd) {
   return x & ~(bad * 0xffffu);
 }
 
-// add_special over the masked stages (from, from + step, ...) of cnt blocks that
-// begin at block j0 with table entries bt: all lanes of a wavefront, for its own
-// columns.  v: LDS for a stage's V of the wavefront's own.
-template <int D, typename C>
+// add_special over the masked ones of a wavefront's stages (steps from, from +
+// step, ... of the walk) of cnt blocks that begin at block j0 with table entries
+// bt: all its lanes, for its own columns.  v: LDS for a stage's V of the wavefront's own.
+template <int D, typename C, typename W>
 __device__ __forceinline__ void special_pass(C& cols, const BiasedParams& p, const int32_t* bt, const uint16_t* vbase,
-                                             int cnt, int j0, int from, int step, int all_lo, int all_hi, lds_u8_t* v,
-                                             lds_f32_t* rowv) {
+                                             const W& walk, int cnt, int j0, int from, int step, int all_lo, int all_hi,
+                                             lds_u8_t* v, lds_f32_t* rowv) {
   constexpr int kChunks = D / 8;
   const int lane = threadIdx.x & 63;
 #pragma unroll 1
-  for (int s = from; 2 * s < cnt; s += step) {
+  for (int i = from; i < walk.n; i += step) {
+    const int s = walk.at(i);
     const int t0 = (j0 + 2 * s) * 16;
     if (t0 >= all_lo && t0 + kTokens <= all_hi) continue;
 #pragma unroll 1
@@ -575,7 +576,7 @@ __device__ __forceinline__ void split_body(const BiasedParams& p, int wg, lds_u8
   }
 
   if (__builtin_amdgcn_ballot_w64(odd != 0) != 0)
-    special_pass<D>(C, p, bt, vbase, cnt, j0, wave, kWaves, all_lo, all_hi, st, rowv);
+    special_pass<D>(C, p, bt, vbase, walk, cnt, j0, wave, kWaves, all_lo, all_hi, st, rowv);
 
   // Merge.  Row n's maximum and sum over the wavefronts, then each wavefront
   // scales its outputs to the common maximum and the final sum; wavefront d
@@ -821,7 +822,7 @@ __device__ __forceinline__ void big_body(const BiasedParams& p, int wg, lds_u8_t
     if (__builtin_amdgcn_ballot_w64(odd != 0) != 0 && lane == 0) flag[wave] = 1;
     __syncthreads();
     if (wave_uniform(flag[0] | flag[1] | flag[2] | flag[3]) != 0)
-      special_pass<D>(C, p, bt, vbase, cnt, j0, 0, 1, all_lo, all_hi, smem + wave * (kBiasedTileRows * D * 2), rowv);
+      special_pass<D>(C, p, bt, vbase, walk, cnt, j0, 0, 1, all_lo, all_hi, smem + wave * (kBiasedTileRows * D * 2), rowv);
   }
 
   // Normalise, transpose through LDS and write bf16 rows in 16-byte pieces.

@@ -234,14 +234,15 @@ def test_rows_that_see_nothing():
     assert (c.run() == 0).all()
 
 
+@pytest.mark.parametrize("alibi", [False, True])
 @pytest.mark.parametrize("d", [64, 128])
 @pytest.mark.parametrize("decode", [True, False])
-def test_infinities_and_nan_in_hidden_places(d, decode):
+def test_infinities_and_nan_in_hidden_places(d, decode, alibi):
     """K and V of tokens that some or all rows do not see hold infinities and NaN; rows that see one show it."""
-    print(f"[gpu case] special values {d} {decode}", flush=True)
+    print(f"[gpu case] special values {d} {decode} {alibi}", flush=True)
     rng = np.random.default_rng(8)
     chunk = [1, 1, 1] if decode else [70, 200, 33]
-    c = Case(6, ctx=[150, 400, 33], chunk=chunk, hq=8, hkv=2, d=d, window=60, cap=0.0 if d == 64 else 30.0)
+    c = Case(6, ctx=[150, 400, 33], chunk=chunk, hq=8, hkv=2, d=d, window=60, cap=0.0 if d == 64 else 30.0, alibi=alibi)
     for b, n in enumerate(c.ctx):
         hidden = n - chunk[b] - 60 + 1                    # below it nobody looks
         for t in range(max(0, hidden)):
@@ -275,6 +276,25 @@ def test_lowest_values_in_visible_places():
     assert np.isnan(x[~fin]).all() or (x[~fin] == 0).all()      # a row that sees -inf alone has no softmax
     ref[~fin] = x[~fin]
     c.check(got, ref, 60.0)
+
+
+@pytest.mark.parametrize("alibi", [False, True])
+@pytest.mark.parametrize("hq,chunks", [(8, [12] * 40), (64, [3, 5, 2])])     # 128 rows per workgroup, 32 over several stages
+def test_special_values_in_both_forms(hq, chunks, alibi):
+    """Infinities and NaN that some rows of a tile see and others do not, in every stage of long contexts."""
+    print(f"[gpu case] special values in both forms {hq} {alibi}", flush=True)
+    ctx = [700 + 17 * i for i in range(len(chunks))] if hq == 64 else [n + 40 for n in chunks]
+    c = Case(15, ctx=ctx, chunk=chunks, hq=hq, hkv=8, d=128, alibi=alibi,
+             docs=lambda c, rng: np.concatenate([rng.integers(0, n - m, m) for n, m in zip(c.ctx, c.chunk)]))
+    rng = np.random.default_rng(3)
+    for b, n in enumerate(c.ctx):
+        for t in rng.integers(0, n, 2):
+            c.v[c.table[b, t // 16], rng.integers(0, 8), t % 16, rng.integers(0, 128)] = rng.choice([NAN, INF, NINF])
+    got = c.run()
+    with np.errstate(all="ignore"):
+        ref = c.reference()
+    assert 0 < (~np.isfinite(ref)).sum() < ref.size // 2
+    c.check(got, ref)
 
 
 @pytest.mark.parametrize("decode", [True, False])
