@@ -135,10 +135,11 @@ __device__ __forceinline__ Row row_of(const BiasedParams& p, const Chunk& c, int
 }
 
 // A raw score capped, in log2 units: within the polynomial's range, and anywhere.
-__device__ __forceinline__ float cap_near(const BiasedParams& p, float x) {
+__device__ __forceinline__ float cap_factor(const BiasedParams& p, float x) {
   const float u = x * x;
-  return x * fmaf(u, fmaf(u, fmaf(u, p.c3, p.c2), p.c1), p.c0);
+  return fmaf(u, fmaf(u, fmaf(u, p.c3, p.c2), p.c1), p.c0);
 }
+__device__ __forceinline__ float cap_near(const BiasedParams& p, float x) { return x * cap_factor(p, x); }
 __device__ __forceinline__ float cap_any(const BiasedParams& p, float x) {
   const float t = fast_exp2(x * p.two_z);
   const float z = fmaf(-2.f * p.cap, __builtin_amdgcn_rcpf(t + 1.f), p.cap);
@@ -154,6 +155,7 @@ struct Columns {
   floatx16_t o[D / 32];         // [j][r]: row 8(r/4) + 4h + r%4, dim 32j + n
   float scale;                  // |scale_log2|
   float base;                   // of the shaped stage (see shape)
+  float most;                   // its largest |raw score| (CAP)
 
   // Operand of step s from the row's memory; bf16 negation is exact.
   static __device__ __forceinline__ u32x4_t query(const BiasedParams& p, const uint16_t* q_row, int s, int h) {
@@ -190,40 +192,50 @@ struct Columns {
     return a;
   }
 
-  // Cap, bias and masks of a stage whose first token is t0; `linear`: no row's
-  // position is before the stage's last token.  Without CAP and BIAS the scores
-  // stay raw; with CAP alone they become log2 units; so with BIAS, in a linear
-  // stage without the part of the bias that all its tokens share, base = slope
+  // Shapes the raw scores of a stage whose first token is t0, in two parts.
+  //
+  // shape: what nearly every stage needs, without a branch, so that the compiler
+  // can place it between the PV MFMAs of the stage before.  Without CAP and BIAS
+  // the scores stay raw; with CAP alone they become log2 units; so with BIAS,
+  // without the part of the bias that all tokens of the stage share, base = slope
   // (t0 + 4h - p): one FMA per score adds slope (t - t0 - 4h), and base goes where
   // the running max does.
-  __device__ __forceinline__ void shape(const BiasedParams& p, floatx16_t& a, int t0, bool edge, bool linear, int h) {
+  //
+  // reshape: the same anew for a stage with a score beyond the polynomial or
+  // tokens after a row's position (not linear: |p - t|); then the masks, in a stage
+  // with hidden tokens (edge).
+  __device__ __forceinline__ floatx16_t shape(const BiasedParams& p, const floatx16_t& raw, int t0, int h) {
+    floatx16_t a = raw;
     if constexpr (CAP) {
-      float most = 0.f;
+      most = fabsf(raw[0]);
 #pragma unroll
-      for (int r = 0; r < 16; ++r) most = fmaxf(most, fabsf(a[r]));
-      if (__builtin_amdgcn_ballot_w64(!(most <= p.raw_max)) != 0) {
+      for (int r = 1; r < 16; ++r) most = fmaxf(most, fabsf(raw[r]));
+    }
+    if constexpr (CAP || BIAS) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) a[r] = cap_any(p, a[r]);
-      } else {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) a[r] = cap_near(p, a[r]);
+      for (int r = 0; r < 16; ++r) {
+        const float off = BIAS ? row.slope * (float)(8 * (r >> 2) + (r & 3)) : 0.f;
+        if constexpr (CAP)
+          a[r] = BIAS ? fmaf(raw[r], cap_factor(p, raw[r]), off) : raw[r] * cap_factor(p, raw[r]);
+        else
+          a[r] = fmaf(raw[r], scale, off);
       }
     }
-    base = 0.f;
-    if constexpr (BIAS) {
-      const float d0 = row.pos - (float)(t0 + 4 * h);
-      if (linear) {
-        base = -row.slope * d0;
+    if constexpr (BIAS) base = row.slope * ((float)(t0 + 4 * h) - row.pos);
+    return a;
+  }
+  __device__ __forceinline__ void reshape(const BiasedParams& p, floatx16_t& a, const floatx16_t& raw, int t0, bool edge,
+                                          bool linear, int h) {
+    if constexpr (CAP || BIAS) {
+      bool again = BIAS && !linear;
+      if constexpr (CAP) again |= __builtin_amdgcn_ballot_w64(!(most <= p.raw_max)) != 0;
+      if (again) {
+        base = 0.f;
+        const float d0 = row.pos - (float)(t0 + 4 * h);
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const float off = row.slope * (float)(8 * (r >> 2) + (r & 3));
-          a[r] = CAP ? a[r] + off : fmaf(a[r], scale, off);
-        }
-      } else {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const float y = CAP ? a[r] : a[r] * scale;
-          a[r] = fmaf(-row.slope, fabsf(d0 - (float)(8 * (r >> 2) + (r & 3))), y);
+          const float y = CAP ? cap_any(p, raw[r]) : raw[r] * scale;
+          a[r] = BIAS ? fmaf(-row.slope, fabsf(d0 - (float)(8 * (r >> 2) + (r & 3))), y) : y;
         }
       }
     }
@@ -569,8 +581,9 @@ __device__ __forceinline__ void split_body(const BiasedParams& p, int wg, lds_u8
       *reinterpret_cast<lds_u32x4_t*>(st + kVOffset<D> + v_off<D>(r, lchunk)) = rv[i];
     }
     load(s + kWaves);
-    floatx16_t a = C.scores(st, h, n, [&](int i) { return ql[64 * i]; });
-    C.shape(p, a, t0, edge, t0 + kTokens <= from_pos + 1, h);
+    const floatx16_t raw = C.scores(st, h, n, [&](int i) { return ql[64 * i]; });
+    floatx16_t a = C.shape(p, raw, t0, h);
+    C.reshape(p, a, raw, t0, edge, t0 + kTokens <= from_pos + 1, h);
     C.raise(a, rowv, h, n);
     C.attend(a, st, lane);
   }
@@ -793,23 +806,25 @@ __device__ __forceinline__ void big_body(const BiasedParams& p, int wg, lds_u8_t
   publish(1, 1);
   load(2);
   __syncthreads();
-  floatx16_t a = C.scores(smem, h, n, query);
-  C.shape(p, a, first_of(0), edge(0), first_of(0) + kTokens <= from_pos + 1, h);
+  auto linear = [&](int s) { return first_of(s) + kTokens <= from_pos + 1; };
+  floatx16_t raw = C.scores(smem, h, n, query);
+  floatx16_t a = C.shape(p, raw, first_of(0), h);
+  C.reshape(p, a, raw, first_of(0), edge(0), linear(0), h);
   C.raise(a, rowv, h, n);
   for (int s0 = 0; s0 < nstage; s0 += kSlots) {
 #pragma unroll
     for (int u = 0; u < kSlots; ++u) {
       const int s = s0 + u;
       if (s < nstage) {                                // uniform over the workgroup
-        floatx16_t next = C.scores(smem + (u + 1) % kSlots * kStageBytes<D>, h, n, query);
+        raw = C.scores(smem + (u + 1) % kSlots * kStageBytes<D>, h, n, query);
         publish(s + 2, (u + 2) % kSlots);
         load(s + 3);
         C.attend(a, smem + u * kStageBytes<D>, lane);
+        a = C.shape(p, raw, first_of(s + 1), h);
         if (s + 1 < nstage) {
-          C.shape(p, next, first_of(s + 1), edge(s + 1), first_of(s + 1) + kTokens <= from_pos + 1, h);
-          C.raise(next, rowv, h, n);
+          C.reshape(p, a, raw, first_of(s + 1), edge(s + 1), linear(s + 1), h);
+          C.raise(a, rowv, h, n);
         }
-        a = next;
         __syncthreads();
       }
     }
