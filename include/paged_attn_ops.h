@@ -167,7 +167,8 @@ int paged_attn_biased_workspace_size(const pa_kv_pool *pool, int32_t batch, int3
  *   q, block_tables, bt_stride, context_lens, batch, scale, max_context_len
  *                    as in paged_attn_decode
  *   num_q_heads      any multiple of the pool's num_kv_heads
- *   softcap          0 (none) or positive, finite
+ *   softcap          0 (none) or positive, finite (PA_EUNSUPPORTED where its
+ *                    ratio to scale leaves the range of fp32)
  *   slopes           device fp32 [num_q_heads], or NULL
  *   window           0 (none) or positive
  *   first_tokens     device int32 [batch], or NULL

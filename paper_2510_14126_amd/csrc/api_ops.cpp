@@ -30,12 +30,15 @@ bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) %
 int64_t type_bytes(int32_t dtype) { return dtype == PA_FP32 ? 4 : 2; }
 
 // Rows of one operand: pointer, stride and the values per token that it must hold.
-int check_rows(const void* x, int64_t stride, int64_t width, int64_t elem, const char* name, const char* fn) {
+int check_rows(const void* x, int64_t stride, int64_t width, int64_t tokens, int64_t elem, const char* name,
+               const char* fn) {
   if (!x) return fail(PA_EINVAL, "%s: %s is NULL", fn, name);
   if (!aligned(x, 16)) return fail(PA_EINVAL, "%s: %s is not 16-byte aligned", fn, name);
   if (stride < width)
     return fail(PA_EINVAL, "%s: %s's stride %lld < heads * head_dim = %lld", fn, name, (long long)stride, (long long)width);
-  if (stride > (int64_t)1 << 40 || stride * elem % 16 != 0)
+  if (stride > ((int64_t)1 << 60) / elem / tokens)
+    return fail(PA_EINVAL, "%s: %s's stride %lld is too large", fn, name, (long long)stride);
+  if (stride * elem % 16 != 0)
     return fail(PA_EINVAL, "%s: %s's stride %lld is not a multiple of 16 bytes", fn, name, (long long)stride);
   return PA_OK;
 }
@@ -159,7 +162,7 @@ int paged_attn_norm_rope(const pa_rope* rope, const void* q, int64_t q_stride, i
       {q, q_stride, num_q_heads, "q"}, {q_out, q_out_stride, num_q_heads, "q_out"},
       {k, k_stride, num_kv_heads, "k"}, {k_out, k_out_stride, num_kv_heads, "k_out"}};
   for (const auto& r : rows)
-    if (r.heads > 0 && (rc = check_rows(r.x, r.stride, (int64_t)r.heads * rope->head_dim, elem, r.name, fn))) return rc;
+    if (r.heads > 0 && (rc = check_rows(r.x, r.stride, (int64_t)r.heads * rope->head_dim, tokens, elem, r.name, fn))) return rc;
   if (!positions || !aligned(positions, 4))
     return fail(PA_EINVAL, "%s: positions is NULL or not 4-byte aligned", fn);
   p.q = q;
@@ -198,11 +201,11 @@ int paged_attn_rope_append(const pa_kv_pool* pool, const pa_rope* rope, const vo
   if (batch == 0 || total_q == 0) return PA_OK;
   const int64_t elem = type_bytes(dtype);
   const int64_t q_width = (int64_t)num_q_heads * pool->head_dim, kv_width = (int64_t)pool->num_kv_heads * pool->head_dim;
-  if (num_q_heads > 0 && (rc = check_rows(q, q_stride, q_width, elem, "q", fn))) return rc;
+  if (num_q_heads > 0 && (rc = check_rows(q, q_stride, q_width, total_q, elem, "q", fn))) return rc;
   if (num_q_heads > 0 && (!q_out || !aligned(q_out, 16)))
     return fail(PA_EINVAL, "%s: q_out is NULL or not 16-byte aligned", fn);
-  if ((rc = check_rows(k, k_stride, kv_width, elem, "k", fn))) return rc;
-  if ((rc = check_rows(v, v_stride, kv_width, elem, "v", fn))) return rc;
+  if ((rc = check_rows(k, k_stride, kv_width, total_q, elem, "k", fn))) return rc;
+  if ((rc = check_rows(v, v_stride, kv_width, total_q, elem, "v", fn))) return rc;
   if (!block_tables || !context_lens)
     return fail(PA_EINVAL, "%s: block_tables and context_lens must be non-NULL", fn);
   if (!aligned(block_tables, 4) || !aligned(context_lens, 4) || !aligned(q_start, 4) || !aligned(positions, 4))
@@ -310,7 +313,8 @@ int plan_biased(const pa_kv_pool* pool, int32_t batch, int32_t num_q_heads, int3
   if (*slots > 0x7fffffffLL / pool->num_kv_heads) return fail(PA_EINVAL, "%s: grid too large", fn);
   *slots *= pool->num_kv_heads;
   *pl = biased_plan(batch, pool->num_kv_heads, group, pool->head_dim, max_context_len, max_chunk, window);
-  if (*slots * pl->parts > 0x7fffffffLL) return fail(PA_EINVAL, "%s: grid too large", fn);
+  if (*slots * pl->parts > 0x7fffffffLL || (pl->parts > 1 && *slots * pl->tile_rows > 0x7fffffffLL))
+    return fail(PA_EINVAL, "%s: grid too large", fn);
   return PA_OK;
 }
 
@@ -385,6 +389,9 @@ int biased_impl(const pa_kv_pool* pool, const void* q, const int32_t* q_start, i
     p.c3 = (float)(kT[3] * s * kLog2e * z * z * z * z * z * z);
     p.raw_max = (float)std::min(0.5 / std::max(z, 1e-30), 1e9);
     p.two_z = (float)(2.0 * kLog2e * z);
+    if (!std::isfinite(p.cap) || !std::isfinite(p.c1) || !std::isfinite(p.c2) || !std::isfinite(p.c3) ||
+        !std::isfinite(p.two_z))
+      return fail(PA_EUNSUPPORTED, "%s: softcap = %g with scale = %g leaves the range of fp32", fn, softcap, scale);
   }
   const hipError_t e = pa::launch_biased(p, static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return fail(PA_EHIP, "%s: kernel launch failed: %s", fn, hipGetErrorString(e));

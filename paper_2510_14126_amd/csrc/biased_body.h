@@ -447,7 +447,7 @@ __device__ __forceinline__ void split_body(const BiasedParams& p, int wg, lds_u8
 
   // Where nothing but the context length bounds what rows see, the partition's
   // first block ids are loaded with it instead of after it.
-  const bool whole = p.window == 0 && p.first_tokens == nullptr;
+  const bool whole = p.window == 0 && p.first_tokens == nullptr && p.bt_stride > 0;
   int ids_first = 0;
   if (whole) {
     const int64_t j = (int64_t)part * p.part_blocks + lane;

@@ -166,7 +166,7 @@ __device__ __forceinline__ void decode_body(const BiasedParams& p, int wg, lds_u
 
   // Where nothing but the context length bounds what the row sees, the
   // partition's first block ids are loaded with it instead of after it.
-  const bool whole = p.window == 0 && p.first_tokens == nullptr;
+  const bool whole = p.window == 0 && p.first_tokens == nullptr && p.bt_stride > 0;
   int ids_first = 0;
   if (whole) ids_first = table[min((int64_t)part * p.part_blocks + lane, (int64_t)p.bt_stride - 1)];
   const int first_token = p.first_tokens ? p.first_tokens[b] : 0;

@@ -326,6 +326,20 @@ def test_bad_device_data_stays_inside(decode):
                 assert (out[0] == 3.0).all() and (out[-1] == 3.0).all() and (ws[size:] == 7).all()
 
 
+@pytest.mark.parametrize("hq", [8, 32])                  # both decode forms
+def test_decode_of_empty_sequences_alone(hq):
+    """No sequence holds a token, and the table has no columns: zeros."""
+    print(f"[gpu case] empty decode {hq}", flush=True)
+    k = torch.full((2, 2, 16, 64), float("nan"), device=DEV, dtype=torch.bfloat16)
+    pool = pa.kv_pool_create(2, 16, 2, 64, k, k)
+    q = torch.ones(3, hq, 64, device=DEV, dtype=torch.bfloat16)
+    ctx, table = dev32([0, 5, -1]), torch.zeros(4, dtype=torch.int32, device=DEV)
+    out = torch.full((3, hq, 64), 7.0, device=DEV, dtype=torch.bfloat16)
+    pa.paged_attn_decode_biased(pool, q, table, 0, ctx, 3, hq, 0.1, 0.0, None, 0, None, 0, None, 0, out)
+    torch.cuda.synchronize()
+    assert (out == 0).all()
+
+
 def test_side_stream_and_two_calls_at_once():
     """Two calls on two streams, each with its workspace, give what each gives alone."""
     print("[gpu case] streams", flush=True)

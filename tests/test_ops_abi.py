@@ -113,7 +113,8 @@ NORM = dict(q=A, q_stride=512, num_q_heads=8, q_weight=A, k=A, k_stride=128, num
     dict(num_q_heads=9), dict(num_q_heads=65537), dict(q_weight=A + 4), dict(k_weight=A + 8), dict(k=None), dict(k=A + 2),
     dict(k_stride=64), dict(num_kv_heads=-2), dict(eps=-1e-6), dict(eps=float("nan")), dict(eps=float("inf")),
     dict(dtype=3), dict(dtype=-1), dict(positions=None), dict(positions=A + 2), dict(tokens=-1), dict(q_out=None),
-    dict(q_out=A + 4), dict(q_out_stride=8), dict(k_out=None), dict(k_out_stride=2 ** 62), dict(k_out_stride=130)], ids=str)
+    dict(q_out=A + 4), dict(q_out_stride=8), dict(k_out=None), dict(k_out_stride=2 ** 62), dict(k_out_stride=130),
+    dict(tokens=2 ** 31 - 1, q_stride=2 ** 40)], ids=str)
 def test_norm_rope_refusals(bad):
     rope = pa.pa_rope_create(64, 64, pa.PA_ROPE_HALF, [1.0] * 32)
     with pytest.raises(pa.PagedAttnError) as e:
@@ -187,6 +188,14 @@ def test_extend_biased_refusals(bad):
     with pytest.raises(pa.PagedAttnError) as e:
         pa.paged_attn_extend_biased(pool, **{**EXTEND, **bad})
     assert e.value.code == pa.PA_EINVAL and "paged_attn_extend_biased" in str(e.value)
+
+
+@pytest.mark.parametrize("cap,scale", [(1e-30, 0.1), (3.0e38, 0.1), (1e-3, 1e30)])
+def test_biased_refuses_caps_beyond_fp32(cap, scale):
+    pool = pa.kv_pool_create(8, 16, 2, 64, A, A)
+    with pytest.raises(pa.PagedAttnError) as e:
+        pa.paged_attn_decode_biased(pool, **{**DECODE, "softcap": cap, "scale": scale})
+    assert e.value.code == pa.PA_EUNSUPPORTED
 
 
 def test_biased_no_ops():
