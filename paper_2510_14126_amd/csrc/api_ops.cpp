@@ -251,25 +251,44 @@ constexpr double kLog2e = 1.4426950408889634;
 // three of 400 over 2704 (1111) 80 / 105, 500 over 2804 (1377) 92 / 114, one prompt of
 // 2000 (1000) 62 / 69, 2600 (1300) 92 / 90, 3000 (1500) 116 / 106.
 //
+// A call's chunks are the bounds max_chunk and max_context_len, or what total_q
+// leaves of them with half a tile more per sequence: ragged chunks hold fewer
+// rows.  128-row form, taken by the bounds alone / 32-row: three chunks of 82, 230
+// and 380 over 2064 tokens, capped, 122 / 84 us; 19 of at most 80 over 7.7K with
+// slopes, 8 heads over 8, 311 / 238 us.
+//
 // Tokens of a 32-row tile: one partition, or several, merged by a second launch
-// (2.5 us), where the tiles alone are fewer workgroups than CUs and hold more
-// than kWholeBlocks blocks each.  One / several partitions, decode, 32 heads over
-// 8: one sequence of 512 tokens 7.0 / 8.7 us, 768 8.9 / 8.5, 1024 10.9 / 8.6;
-// twice as many workgroups: one of 30011 28.0 / 28.0, eight of 4096 23.9 / 26.0.
+// (2.5 us), where the tiles alone are few workgroups and hold more than
+// kWholeBlocks blocks each.  One / several partitions, decode, 32 heads over 8: one
+// sequence of 512 tokens 7.0 / 8.7 us, 768 8.9 / 8.5, 1024 10.9 / 8.6.  As many as
+// keep the grid within one workgroup per CU, at D = 64, whose workgroups read half
+// as much, within two; at most 256 / 512 / 768 workgroups, decode: D = 128, four
+// sequences of 16384 tokens, 32 heads over 8, 43.2 / 44.4 / 45.6 us, 4096 13.6 /
+// 13.9 / 14.2, three of 10000, 16 over 8, 22.0 / 22.6 / 23.4 (27.1 at 264, a few
+// more than the CUs); D = 64, eight of 8192, 32 over 8, 28.0 / 23.5 / 25.2, 16 of
+// 4096, 32 over 4, 16.4 / 14.3 / 15.9, four of 9000, 12 over 12, 25.4 / 20.6 / 21.5.
+// The bounds alone decide them, as they decide the workspace.
+//
 // In a decode, whose contexts differ, a partition holds at most kMostBlocks: 256
 // of 64..8192 tokens in partitions of at most 64 / 96 / 128 blocks 269 / 265 / 265
 // us, 64 with a window of 4096 169 / 168 / 167, of 32 blocks 303 / 175.
-constexpr int64_t kFillWorkgroups = 256;
+constexpr int64_t kFillWorkgroups128 = 256, kFillWorkgroups64 = 512;
 constexpr int64_t kWholeBlocks = 40, kLeastBlocks = 16, kMostBlocks = 128;
-pa::BiasedPlan biased_plan(int batch, int num_kv_heads, int group, int head_dim, int max_ctx, int max_chunk, int window) {
+
+pa::BiasedPlan biased_plan(int batch, int num_kv_heads, int group, int head_dim, int max_ctx, int max_chunk, int window,
+                           int64_t total_q) {
   pa::BiasedPlan pl;
   const int64_t rows = (int64_t)std::max(max_chunk, 1) * group;
   const int64_t tiles = (rows + pa::kBiasedTileRows - 1) / pa::kBiasedTileRows;
   const int64_t big_tiles = (rows + pa::kBiasedWgRows - 1) / pa::kBiasedWgRows;
   const int64_t wgs = std::max<int64_t>(1, batch * tiles * num_kv_heads), big_wgs = batch * big_tiles * num_kv_heads;
-  const double resident = head_dim == 64 ? 1280 : 896;
-  pl.big = max_chunk > 1 && wgs > 2 * big_wgs &&
-           wgs * (2.0 * max_ctx - max_chunk) > 2.0 * resident * max_ctx;
+  auto long_chunks = [&](int64_t n32, int64_t n128) {
+    return max_chunk > 1 && n32 > 2 * n128 &&
+           n32 * (2.0 * max_ctx - max_chunk) > 2.0 * (head_dim == 64 ? 1280 : 896) * max_ctx;
+  };
+  auto tiles_of = [&](int64_t rows_per) { return (total_q * group / rows_per + (batch + 1) / 2) * num_kv_heads; };
+  pl.big = long_chunks(wgs, big_wgs) &&
+           long_chunks(std::min(wgs, tiles_of(pa::kBiasedTileRows)), std::min(big_wgs, tiles_of(pa::kBiasedWgRows)));
   pl.tiles = (int32_t)(pl.big ? big_tiles : tiles);
   pl.tile_rows = (int32_t)std::min<int64_t>(rows, pa::kBiasedTileRows);
   const int64_t all = ((int64_t)max_ctx + PA_BLOCK_SIZE - 1) / PA_BLOCK_SIZE;
@@ -277,7 +296,9 @@ pa::BiasedPlan biased_plan(int batch, int num_kv_heads, int group, int head_dim,
   const int64_t blocks = window > 0 ? std::min(all, ((int64_t)window + pa::kBiasedTileRows / group + PA_BLOCK_SIZE - 1) / PA_BLOCK_SIZE + 1) : all;
   int64_t per = blocks;
   if (!pl.big && blocks > kWholeBlocks) {
-    per = std::max(kLeastBlocks, (blocks * wgs / kFillWorkgroups + 1) / 2 * 2);
+    const int64_t fill = head_dim == 64 ? kFillWorkgroups64 : kFillWorkgroups128;
+    const int64_t parts = std::max<int64_t>(1, fill / wgs);
+    per = std::max(kLeastBlocks, (blocks + 2 * parts - 1) / (2 * parts) * 2);
     if (max_chunk <= 1) per = std::min(per, kMostBlocks);
   }
   per = std::max<int64_t>(per, 1);
@@ -295,7 +316,7 @@ size_t biased_lse_bytes(const pa::BiasedPlan& pl, int64_t slots) {
 
 // Geometry and plan of a biased call, and its number of row tiles.
 int plan_biased(const pa_kv_pool* pool, int32_t batch, int32_t num_q_heads, int32_t max_context_len,
-                int32_t max_chunk, int32_t window, pa::BiasedPlan* pl, int64_t* slots, const char* fn) {
+                int32_t max_chunk, int32_t window, int64_t total_q, pa::BiasedPlan* pl, int64_t* slots, const char* fn) {
   if (!pool) return fail(PA_EINVAL, "%s: pool is NULL", fn);
   if (batch < 0) return fail(PA_EINVAL, "%s: batch = %d < 0", fn, batch);
   if (num_q_heads <= 0 || num_q_heads % pool->num_kv_heads != 0)
@@ -312,7 +333,8 @@ int plan_biased(const pa_kv_pool* pool, int32_t batch, int32_t num_q_heads, int3
   *slots = (int64_t)batch * tiles;
   if (*slots > 0x7fffffffLL / pool->num_kv_heads) return fail(PA_EINVAL, "%s: grid too large", fn);
   *slots *= pool->num_kv_heads;
-  *pl = biased_plan(batch, pool->num_kv_heads, group, pool->head_dim, max_context_len, max_chunk, window);
+  *pl = biased_plan(batch, pool->num_kv_heads, group, pool->head_dim, max_context_len, max_chunk, window,
+                    total_q);
   if (*slots * pl->parts > 0x7fffffffLL || (pl->parts > 1 && *slots * pl->tile_rows > 0x7fffffffLL))
     return fail(PA_EINVAL, "%s: grid too large", fn);
   return PA_OK;
@@ -325,7 +347,7 @@ int biased_impl(const pa_kv_pool* pool, const void* q, const int32_t* q_start, i
                 void* workspace, size_t workspace_bytes, void* out, void* stream, const char* fn) {
   pa::BiasedPlan pl;
   int64_t slots = 0;
-  int rc = plan_biased(pool, batch, num_q_heads, max_context_len, max_chunk, window, &pl, &slots, fn);
+  int rc = plan_biased(pool, batch, num_q_heads, max_context_len, max_chunk, window, total_q, &pl, &slots, fn);
   if (rc) return rc;
   if (total_q < 0) return fail(PA_EINVAL, "%s: total_q = %d < 0", fn, total_q);
   const int64_t need_bt = ((int64_t)max_context_len + PA_BLOCK_SIZE - 1) / PA_BLOCK_SIZE;
@@ -406,7 +428,7 @@ int paged_attn_biased_workspace_size(const pa_kv_pool* pool, int32_t batch, int3
   if (!bytes_out) return fail(PA_EINVAL, "%s: NULL output pointer", fn);
   pa::BiasedPlan pl;
   int64_t slots = 0;
-  const int rc = plan_biased(pool, batch, num_q_heads, max_context_len, max_chunk, window, &pl, &slots, fn);
+  const int rc = plan_biased(pool, batch, num_q_heads, max_context_len, max_chunk, window, 0, &pl, &slots, fn);
   if (rc) return rc;
   *bytes_out = biased_part_o_bytes(pl, slots, pool->head_dim) + biased_lse_bytes(pl, slots);
   return PA_OK;
