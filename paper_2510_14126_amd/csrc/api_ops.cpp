@@ -245,11 +245,11 @@ constexpr double kLog2e = 1.4426950408889634;
 // those, weighed by the tokens a chunk's average row sees against the longest
 // context, are few, or while they are at most twice the others, whose tiles are
 // then mostly empty.  32-row / 128-row form, capped, 32 heads over 8, weighed
-// workgroups in brackets: D = 128, three chunks of 100 over 2404 tokens (306) 49 /
-// 101 us, of 300 over 2604 (859) 103 / 111, of 600 over 2904 (1610) 189 / 155, one
-// prompt of 1500 (752) 62 / 68, 2000 (1000) 98 / 91, 8191 (4096) 1140 / 881; D = 64,
-// three of 400 over 2704 (1111) 80 / 105, 500 over 2804 (1377) 92 / 114, one prompt of
-// 2000 (1000) 62 / 69, 2600 (1300) 92 / 90, 3000 (1500) 116 / 106.
+// workgroups in brackets: D = 128, three chunks of 100 over 2404 tokens (306) 47 /
+// 81 us, of 300 over 2604 (859) 103 / 94, of 600 over 2904 (1614) 193 / 155, one
+// prompt of 1500 (752) 59 / 58, 2000 (1000) 92 / 78, 8191 (4096) 1149 / 845; D = 64,
+// three of 400 over 2704 (1111) 80 / 98, 500 over 2804 (1377) 95 / 104, one prompt of
+// 2000 (1000) 61 / 55, 2600 (1300) 92 / 75, 3000 (1500) 112 / 91.
 //
 // A call's chunks are the bounds max_chunk and max_context_len, or what total_q
 // leaves of them with half a tile more per sequence: ragged chunks hold fewer
@@ -284,7 +284,7 @@ pa::BiasedPlan biased_plan(int batch, int num_kv_heads, int group, int head_dim,
   const int64_t wgs = std::max<int64_t>(1, batch * tiles * num_kv_heads), big_wgs = batch * big_tiles * num_kv_heads;
   auto long_chunks = [&](int64_t n32, int64_t n128) {
     return max_chunk > 1 && n32 > 2 * n128 &&
-           n32 * (2.0 * max_ctx - max_chunk) > 2.0 * (head_dim == 64 ? 1280 : 896) * max_ctx;
+           n32 * (2.0 * max_ctx - max_chunk) > 2.0 * (head_dim == 64 ? 1280 : 768) * max_ctx;
   };
   auto tiles_of = [&](int64_t rows_per) { return (total_q * group / rows_per + (batch + 1) / 2) * num_kv_heads; };
   pl.big = long_chunks(wgs, big_wgs) &&

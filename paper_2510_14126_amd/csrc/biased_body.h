@@ -370,7 +370,7 @@ struct Columns {
 // The order of a range's stages: with a distance bias from the nearest tokens to
 // the farthest, so that the running max is found first (upwards it rises with
 // every stage of a steep head, and each rise rescales the outputs: a prompt of
-// 8191 tokens upwards 881 us, downwards 779).  at(s): stage of step s (past the last step
+// 8191 tokens upwards 858 us, downwards 726).  at(s): stage of step s (past the last step
 // the last stage again); chunk(s): which 64 blocks hold it.
 template <bool DOWN>
 struct Walk {
