@@ -353,7 +353,8 @@ int biased_impl(const pa_kv_pool* pool, const void* q, const int32_t* q_start, i
   const int64_t need_bt = ((int64_t)max_context_len + PA_BLOCK_SIZE - 1) / PA_BLOCK_SIZE;
   if (bt_stride < need_bt || bt_stride < 0)
     return fail(PA_EINVAL, "%s: bt_stride = %d < ceil(max_context_len / 16) = %lld", fn, bt_stride, (long long)need_bt);
-  if (!std::isfinite(scale)) return fail(PA_EINVAL, "%s: scale is not finite", fn);
+  if (!std::isfinite((float)(scale * kLog2e)))
+    return fail(PA_EINVAL, "%s: scale is not finite, or not in log2 units", fn);
   if (!(softcap >= 0.f) || !std::isfinite(softcap))
     return fail(PA_EINVAL, "%s: softcap is negative or not finite", fn);
   if (batch == 0 || total_q == 0 || max_chunk == 0) return PA_OK;

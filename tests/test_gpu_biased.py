@@ -203,6 +203,8 @@ EXTENDS = {
     "beyond_8192": dict(ctx=[8700], chunk=[140], hq=4, hkv=1, d=128, window=8300),
     "many_tiles": dict(ctx=[500] * 12, chunk=[260] * 12, hq=32, hkv=8, d=128, cap=30.0, qscale=4.0),
     "many_tiles_64": dict(ctx=[420] * 12, chunk=[200] * 12, hq=32, hkv=8, d=64, alibi=True, docs=documents(20, 300)),
+    "many_tiles_rising": dict(ctx=[600] * 12, chunk=[260] * 12, hq=32, hkv=8, d=128, cap=50.0, qscale=8.0),
+    "one_long_of_four": dict(ctx=[900, 5, 700, 2], chunk=[600, 1, 3, 0], hq=32, hkv=8, d=128, cap=50.0, qscale=8.0, pad=2),
     "negative_scale": dict(ctx=[150], chunk=[150], hq=8, hkv=2, d=128, scale=-0.1),
     "zero_scale": dict(ctx=[150], chunk=[150], hq=8, hkv=2, d=128, scale=0.0, window=33),
 }

@@ -164,7 +164,7 @@ EXTEND = dict(q=A, q_start=A, total_q=9, block_tables=A, bt_stride=8, context_le
               workspace=A, workspace_bytes=1 << 30, out=A)
 COMMON = [dict(q=None), dict(q=A + 8), dict(block_tables=None), dict(block_tables=A + 1), dict(bt_stride=6),
           dict(bt_stride=-1), dict(context_lens=None), dict(context_lens=A + 2), dict(batch=-1), dict(num_q_heads=0),
-          dict(num_q_heads=7), dict(scale=float("nan")), dict(scale=float("inf")), dict(softcap=-1.0),
+          dict(num_q_heads=7), dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=-3.0e38), dict(softcap=-1.0),
           dict(softcap=float("nan")), dict(softcap=float("inf")), dict(slopes=A + 2), dict(window=-1),
           dict(first_tokens=A + 1), dict(max_context_len=-1), dict(out=None), dict(out=A + 4)]
 LONG = dict(bt_stride=4096, max_context_len=65536)      # split: needs a workspace
