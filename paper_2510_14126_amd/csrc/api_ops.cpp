@@ -246,10 +246,10 @@ constexpr double kLog2e = 1.4426950408889634;
 // context, are few, or while they are at most twice the others, whose tiles are
 // then mostly empty.  32-row / 128-row form, capped, 32 heads over 8, weighed
 // workgroups in brackets: D = 128, three chunks of 100 over 2404 tokens (306) 47 /
-// 81 us, of 300 over 2604 (859) 103 / 94, of 600 over 2904 (1614) 193 / 155, one
-// prompt of 1500 (752) 59 / 58, 2000 (1000) 92 / 78, 8191 (4096) 1149 / 845; D = 64,
-// three of 400 over 2704 (1111) 80 / 98, 500 over 2804 (1377) 95 / 104, one prompt of
-// 2000 (1000) 61 / 55, 2600 (1300) 92 / 75, 3000 (1500) 112 / 91.
+// 81 us, of 300 over 2604 (859) 97 / 93, of 600 over 2904 (1614) 186 / 144, one
+// prompt of 1500 (752) 57 / 56, 2000 (1000) 89 / 74, 8191 (4096) 1149 / 845; D = 64,
+// three of 400 over 2704 (1111) 77 / 91, 500 over 2804 (1377) 91 / 95, one prompt of
+// 2000 (1000) 58 / 55, 2600 (1300) 90 / 76, 3000 (1500) 112 / 91.
 //
 // A call's chunks are the bounds max_chunk and max_context_len, or what total_q
 // leaves of them with half a tile more per sequence: ragged chunks hold fewer
@@ -395,6 +395,9 @@ int biased_impl(const pa_kv_pool* pool, const void* q, const int32_t* q_start, i
   p.total_q = total_q;
   p.window = window;
   p.big = pl.big;
+  // more than one workgroup per CU and at most two; a chunk's last tile may be part of one
+  const int64_t full = (int64_t)total_q * p.group / pa::kBiasedWgRows, cus = pa::kCus / pool->num_kv_heads;
+  p.ranked = pl.big && batch <= 64 && cus > 0 && full > cus && full + batch <= 2 * cus;
   p.tiles = pl.tiles;
   p.parts = pl.parts;
   p.part_blocks = pl.part_blocks;

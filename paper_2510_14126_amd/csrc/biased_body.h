@@ -702,6 +702,65 @@ template <int D> constexpr int kBigLdsBytes = kBigRange<D> + 4 * kWaves * 4;
 static_assert(kWaves * kBiasedTileRows * 128 * 2 <= kBigRow<128> && kWaves * kBiasedTileRows * 64 * 2 <= kBigRow<64>,
               "the stages' room holds the outputs, and a V tile per wavefront");
 
+// F over the wavefront, of two values at a time; every lane receives it.
+template <typename F>
+__device__ __forceinline__ int all64(int x, F&& f) {
+  x = f(x, dpp_i<kDppQuadXor1>(x));
+  x = f(x, dpp_i<kDppQuadXor2>(x));
+  x = f(x, dpp_i<kDppRowRor4>(x));
+  x = f(x, dpp_i<kDppRowRor8>(x));
+  const auto y = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  x = f((int)y[0], (int)y[1]);
+  const auto z = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return wave_uniform(f((int)z[0], (int)z[1]));
+}
+
+// The order of the row tiles of a call that the GPU holds all at once (ranked):
+// its CUs take one or two workgroups each, and the one with the most work ends the
+// call.  Workgroup w and the one a CU further, w + kCus, share a CU (the
+// dispatcher deals them out in turn), so the tiles that see the most tokens go to
+// the CUs with one and the others in pairs of the longest with the shortest.
+// Sequence after sequence / ranked, capped, D = 128: chunks of 128, 576 and 1024
+// tokens over 2304 resident ones (432 workgroups) 165 / 152 us, four of 600 over
+// 1000, 16 heads over 16 (304), 78 / 65, 17 of 168 over 2432, 12 over 2 (272), 122 /
+// 117.  With more workgroups than slots the sequences' own order is kept:
+// neighbours share their tokens in L2 (four chunks of 3001..4096 tokens in
+// documents ranked by length 201 -> 229 us).
+//
+// Here tile i of a KV head: sequence b, its chunk and tile, false: there are fewer.
+// One sequence per lane; a tile's length counts in tiles, `first` before its chunk.
+__device__ __forceinline__ bool ranked_tile(const BiasedParams& p, int i, int& b, Chunk& c, int& tile) {
+  const int lane = threadIdx.x & 63;
+  const Chunk own = chunk_of(p, min(lane, p.batch - 1));
+  const int tiles = lane < p.batch ? (int)(((int64_t)own.len * p.group + kBiasedWgRows - 1) / kBiasedWgRows) : 0;
+  const int first = (int)min((int64_t)own.first * p.group / kBiasedWgRows, (int64_t)1 << 29);
+  auto sum = [](int x, int y) { return x + y; };
+  const int n = all64(tiles, sum);
+  if (i >= n) return false;
+  const int cus = kCus / p.num_kv_heads;               // tiles of a head until each CU has a workgroup
+  if (n > cus) {
+    const int alone = max(2 * cus - n, 0);             // CUs (tiles of a head) with one workgroup
+    i = i >= cus ? n - 1 - (i - cus) : (i < cus - alone ? alone + i : i - (cus - alone));
+  }
+  auto at_least = [&](int v) { return all64(min(max(first + tiles - v + 1, 0), tiles), sum); };
+  // the largest length v that more than i tiles reach
+  int v = 1, past = all64(first + tiles, [](int x, int y) { return max(x, y); }) + 1;
+  while (past - v > 1) {
+    const int mid = v + (past - v) / 2;
+    if (at_least(mid) > i)
+      v = mid;
+    else
+      past = mid;
+  }
+  uint64_t with = __builtin_amdgcn_ballot_w64(first < v && v <= first + tiles);
+  for (int j = i - at_least(v + 1); j > 0; --j) with &= with - 1;
+  b = __builtin_ctzll(with);
+  tile = v - 1 - __builtin_amdgcn_readlane(first, b);
+  c = {__builtin_amdgcn_readlane(own.start, b), __builtin_amdgcn_readlane(own.len, b),
+       __builtin_amdgcn_readlane(own.first, b), __builtin_amdgcn_readlane(own.ctx, b)};
+  return true;
+}
+
 template <int D, bool CAP, bool BIAS>
 __device__ __forceinline__ void big_body(const BiasedParams& p, int wg, lds_u8_t* smem) {
   const int lane = threadIdx.x & 63;
@@ -712,9 +771,14 @@ __device__ __forceinline__ void big_body(const BiasedParams& p, int wg, lds_u8_t
   const int g = wg % p.num_kv_heads;
   wg /= p.num_kv_heads;
   // A chunk's last rows see the most tokens: they start first.
-  const int tile = p.tiles - 1 - wg % p.tiles;
-  const int b = wg / p.tiles;
-  const Chunk c = chunk_of(p, b);
+  int tile = p.tiles - 1 - wg % p.tiles;
+  int b = wg / p.tiles;
+  Chunk c;
+  if (p.ranked) {
+    if (!ranked_tile(p, wg, b, c, tile)) return;       // whole workgroup
+  } else {
+    c = chunk_of(p, b);
+  }
   const int rows = c.len * p.group;
   if (tile * kBiasedWgRows >= rows) return;            // whole workgroup: no rows here
   const int row0 = tile * kBiasedWgRows + kBiasedTileRows * wave;

@@ -73,6 +73,7 @@ struct BiasedParams {
   int32_t total_q;
   int32_t window;                // 0: none
   int32_t big;                   // 1: kBiasedWgRows rows per workgroup, 0: kBiasedTileRows
+  int32_t ranked;                // big: 1: the GPU holds all workgroups at once, paired by length (batch <= 64)
   int32_t tiles;                 // row tiles (of that many rows) per sequence in the grid
   int32_t parts;                 // partitions of a tile's tokens in the grid
   int32_t part_blocks;           // blocks of a partition (even), where there are several
@@ -88,6 +89,7 @@ struct BiasedParams {
 };
 constexpr int kBiasedTileRows = 32;     // query rows (token x head) of a row tile
 constexpr int kBiasedWgRows = 128;      // rows of a workgroup in the form for long chunks
+constexpr int kCus = 256;               // compute units of the GPU
 
 // Rows and token partitions of a call (kernel launch and workspace size).
 struct BiasedPlan {

@@ -204,6 +204,9 @@ EXTENDS = {
     "many_tiles": dict(ctx=[500] * 12, chunk=[260] * 12, hq=32, hkv=8, d=128, cap=30.0, qscale=4.0),
     "many_tiles_64": dict(ctx=[420] * 12, chunk=[200] * 12, hq=32, hkv=8, d=64, alibi=True, docs=documents(20, 300)),
     "many_tiles_rising": dict(ctx=[600] * 12, chunk=[260] * 12, hq=32, hkv=8, d=128, cap=50.0, qscale=8.0),
+    "paired_tiles": dict(ctx=[900, 700, 0, 1300, 40], chunk=[500, 330, 0, 650, 3], hq=32, hkv=8, d=128, cap=30.0, qscale=4.0),
+    "paired_tiles_64": dict(ctx=[2500, 200, 2400], chunk=[900, 90, 880], hq=30, hkv=6, d=64, alibi=True, pad=9),
+    "paired_tiles_window": dict(ctx=[800] * 7, chunk=[500, 450, 1, 480, 380, 422, 199], hq=16, hkv=16, d=128, window=333),
     "one_long_of_four": dict(ctx=[900, 5, 700, 2], chunk=[600, 1, 3, 0], hq=32, hkv=8, d=128, cap=50.0, qscale=8.0, pad=2),
     "negative_scale": dict(ctx=[150], chunk=[150], hq=8, hkv=2, d=128, scale=-0.1),
     "zero_scale": dict(ctx=[150], chunk=[150], hq=8, hkv=2, d=128, scale=0.0, window=33),
