@@ -293,6 +293,7 @@ pa::BiasedPlan biased_plan(int batch, int num_kv_heads, int group, int head_dim,
   pl.tile_rows = (int32_t)std::min<int64_t>(rows, pa::kBiasedTileRows);
   const int64_t all = ((int64_t)max_ctx + PA_BLOCK_SIZE - 1) / PA_BLOCK_SIZE;
   // a window spans its own tokens and those between a tile's first and last row, wherever they begin in a block
+  // (what a prefix adds to it lengthens the partitions in the kernel, see partition_blocks)
   const int64_t blocks = window > 0 ? std::min(all, ((int64_t)window + pa::kBiasedTileRows / group + PA_BLOCK_SIZE - 1) / PA_BLOCK_SIZE + 1) : all;
   int64_t per = blocks;
   if (!pl.big && blocks > kWholeBlocks) {

@@ -76,7 +76,7 @@ struct BiasedParams {
   int32_t ranked;                // big: 1: the GPU holds all workgroups at once, paired by length (batch <= 64)
   int32_t tiles;                 // row tiles (of that many rows) per sequence in the grid
   int32_t parts;                 // partitions of a tile's tokens in the grid
-  int32_t part_blocks;           // blocks of a partition (even), where there are several
+  int32_t part_blocks;           // blocks of a partition (even), where there are several; see partition_blocks
   int32_t tile_rows;             // rows of a tile that the partial buffers hold
   int32_t stream_tiles;          // 1: load the tiles with the streaming cache hint
   float scale_log2;              // scale * log2(e)
@@ -90,6 +90,17 @@ struct BiasedParams {
 constexpr int kBiasedTileRows = 32;     // query rows (token x head) of a row tile
 constexpr int kBiasedWgRows = 128;      // rows of a workgroup in the form for long chunks
 constexpr int kCus = 256;               // compute units of the GPU
+
+// Blocks of one partition of a row tile that sees nblk blocks.  The plan's
+// part_blocks reach a window and the positions of a tile's rows; a prefix that sees
+// itself whole adds up to the rest of the chunk, and its tiles take longer
+// partitions, in the same number.
+__host__ __device__ inline int partition_blocks(const BiasedParams& p, int nblk) {
+  if (p.parts == 1) return nblk;
+  if (p.prefix_lens == nullptr || p.window == 0) return p.part_blocks;
+  const int even = (int)((nblk + 2 * (int64_t)p.parts - 1) / (2 * (int64_t)p.parts)) * 2;
+  return even > p.part_blocks ? even : p.part_blocks;
+}
 
 // Rows and token partitions of a call (kernel launch and workspace size).
 struct BiasedPlan {
