@@ -190,7 +190,7 @@ __device__ __forceinline__ void decode_body(const BiasedParams& p, int wg, lds_u
   lo = min(max(lo, first_token), hi);
   const int first = lo >> 4;
   const int nblk = hi > lo ? ((hi + 15) >> 4) - first : 0;
-  const int per = partition_blocks(p, nblk);
+  const int per = p.parts == 1 ? nblk : p.part_blocks;
   const int j0 = first + part * per;
   const int cnt = min(per, nblk - part * per);
   const size_t slot = ((size_t)b * p.num_kv_heads + g) * p.parts + part;

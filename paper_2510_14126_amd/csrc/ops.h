@@ -98,7 +98,8 @@ constexpr int kCus = 256;               // compute units of the GPU
 __host__ __device__ inline int partition_blocks(const BiasedParams& p, int nblk) {
   if (p.parts == 1) return nblk;
   if (p.prefix_lens == nullptr || p.window == 0) return p.part_blocks;
-  const int even = (int)((nblk + 2 * (int64_t)p.parts - 1) / (2 * (int64_t)p.parts)) * 2;
+  const uint32_t two = 2u * (uint32_t)p.parts;          // parts < 2^24, blocks <= 2^27: no overflow
+  const int even = (int)(((uint32_t)nblk + two - 1) / two) * 2;
   return even > p.part_blocks ? even : p.part_blocks;
 }
 
