@@ -140,10 +140,14 @@ __device__ __forceinline__ float cap_factor(const BiasedParams& p, float x) {
   return fmaf(u, fmaf(u, fmaf(u, p.c3, p.c2), p.c1), p.c0);
 }
 __device__ __forceinline__ float cap_near(const BiasedParams& p, float x) { return x * cap_factor(p, x); }
-__device__ __forceinline__ float cap_any(const BiasedParams& p, float x) {
+__device__ __forceinline__ float cap_far(const BiasedParams& p, float x) {
   const float t = fast_exp2(x * p.two_z);
-  const float z = fmaf(-2.f * p.cap, __builtin_amdgcn_rcpf(t + 1.f), p.cap);
-  return fabsf(x) <= p.raw_max ? cap_near(p, x) : z;
+  return fmaf(-2.f * p.cap, __builtin_amdgcn_rcpf(t + 1.f), p.cap);
+}
+__device__ __forceinline__ bool cap_is_near(const BiasedParams& p, float x) { return fabsf(x) <= p.raw_max; }
+__device__ __forceinline__ float cap_any(const BiasedParams& p, float x) {
+  const float z = cap_far(p, x);
+  return cap_is_near(p, x) ? cap_near(p, x) : z;
 }
 
 // The 32 columns of one wavefront: queries (Q^T operand of step s: dims 16s + 8h
@@ -202,9 +206,10 @@ struct Columns {
   // slope (t0 + 4h - p): one FMA per score adds slope (t - t0 - 4h), and base goes
   // where the running max does.
   //
-  // reshape: the same anew for a stage with a score beyond the polynomial or
-  // tokens after a row's position (not linear: |p - t|); then the masks, in a stage
-  // with hidden tokens (edge).
+  // reshape: in a stage with scores beyond the polynomial those alone anew, so that
+  // no score's bits depend on another, which its row may not see; in one with
+  // tokens after a row's position (not linear) what |p - t| is more than p - t, twice
+  // t - p; then the masks, in a stage with hidden tokens (edge).
   __device__ __forceinline__ floatx16_t shape(const BiasedParams& p, const floatx16_t& raw, int t0, int h) {
     floatx16_t a = raw;
     if constexpr (CAP) {
@@ -224,18 +229,17 @@ struct Columns {
   }
   __device__ __forceinline__ void reshape(const BiasedParams& p, floatx16_t& a, const floatx16_t& raw, int t0, bool edge,
                                           bool linear, int h) {
-    if constexpr (CAP || BIAS) {
-      bool again = BIAS && !linear;
-      if constexpr (CAP) again |= __builtin_amdgcn_ballot_w64(!(most <= p.raw_max)) != 0;
-      if (again) {
-        if (BIAS) base = 0.f;
-        const float d0 = row.pos - (float)(t0 + 4 * h);
+    if (CAP && __builtin_amdgcn_ballot_w64(!(most <= p.raw_max)) != 0) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const float y = CAP ? cap_any(p, raw[r]) : raw[r] * scale;
-          a[r] = BIAS ? fmaf(-row.slope, fabsf(d0 - (float)(8 * (r >> 2) + (r & 3))), y) : y - base;
-        }
+      for (int r = 0; r < 16; ++r) {
+        const float z = cap_far(p, raw[r]) + (BIAS ? row.slope * (float)(8 * (r >> 2) + (r & 3)) : neg);
+        a[r] = cap_is_near(p, raw[r]) ? a[r] : z;
       }
+    }
+    if (BIAS && !linear) {
+      const float d0 = row.pos - (float)(t0 + 4 * h);
+#pragma unroll
+      for (int r = 0; r < 16; ++r) a[r] = fmaf(2.f * row.slope, fminf(d0 - (float)(8 * (r >> 2) + (r & 3)), 0.f), a[r]);
     }
     if (edge) {
       // bit k: the row sees token t0 + 4h + k
