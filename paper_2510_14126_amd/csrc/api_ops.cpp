@@ -9,6 +9,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <new>
 
@@ -409,15 +410,22 @@ int biased_impl(const pa_kv_pool* pool, const void* q, const int32_t* q_start, i
     // tanh(z) / z on |z| <= 1/2 as a polynomial in z^2, z = raw * |scale| / softcap
     constexpr double kT[4] = {0.9999994557709386, -0.33326317935941446, 0.1319029660321076, -0.04440222612772746};
     const double s = std::fabs((double)scale), z = s / softcap;
+    double c[4], reach = 0.5;
+    for (int i = 3; i >= 0; --i) {
+      c[i] = kT[i] * s * kLog2e * std::pow(z, 2 * i);
+      // a coefficient below fp32's normal numbers: only as far as its term is below 2^-23
+      if (i > 0 && std::fabs(c[i]) < FLT_MIN) reach = std::pow(0x1p-23 / std::fabs(kT[i]), 0.5 / i);
+    }
+    constexpr double kMostRaw = 1e19;                  // its square is finite in fp32
     p.cap = (float)(softcap * kLog2e);
-    p.c0 = (float)(kT[0] * s * kLog2e);
-    p.c1 = (float)(kT[1] * s * kLog2e * z * z);
-    p.c2 = (float)(kT[2] * s * kLog2e * z * z * z * z);
-    p.c3 = (float)(kT[3] * s * kLog2e * z * z * z * z * z * z);
-    p.raw_max = (float)std::min(0.5 / std::max(z, 1e-30), 1e9);
+    p.c0 = (float)c[0];
+    p.c1 = (float)c[1];
+    p.c2 = (float)c[2];
+    p.c3 = (float)c[3];
+    p.raw_max = (float)std::min(reach / std::max(z, 1e-30), kMostRaw);
     p.two_z = (float)(2.0 * kLog2e * z);
     if (!std::isfinite(p.cap) || !std::isfinite(p.c1) || !std::isfinite(p.c2) || !std::isfinite(p.c3) ||
-        !std::isfinite(p.two_z))
+        !std::isfinite(p.two_z) || (s > 0.0 && reach / z > kMostRaw))
       return fail(PA_EUNSUPPORTED, "%s: softcap = %g with scale = %g leaves the range of fp32", fn, softcap, scale);
   }
   const hipError_t e = pa::launch_biased(p, static_cast<hipStream_t>(stream));

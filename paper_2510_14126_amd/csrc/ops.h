@@ -81,7 +81,8 @@ struct BiasedParams {
   int32_t stream_tiles;          // 1: load the tiles with the streaming cache hint
   float scale_log2;              // scale * log2(e)
   // softcap > 0, scores in log2 units x = raw * |scale_log2|: y = raw * (c0 + c1 raw^2
-  // + c2 raw^4 + c3 raw^6) while |raw| <= raw_max, cap - 2 cap / (2^(raw * two_z) + 1) above
+  // + c2 raw^4 + c3 raw^6) while |raw| <= raw_max (|z| <= 1/2, or as far as coefficients
+  // that fp32 holds reach), cap - 2 cap / (2^(raw * two_z) + 1) above
   float cap;                     // softcap * log2(e), or 0
   float c0, c1, c2, c3;
   float raw_max;
