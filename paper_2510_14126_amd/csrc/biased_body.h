@@ -116,7 +116,7 @@ __device__ __forceinline__ Chunk chunk_of(const BiasedParams& p, int b) {
 // What the row of column n sees, and its bias.
 struct Row {
   int lo, hi;       // tokens lo <= t < hi; hi <= lo: none
-  float pos;
+  int pos;          // differences of positions become fp32, not positions: those pass 2^24
   float slope;      // log2 units per token of distance
 };
 template <bool BIAS>
@@ -129,7 +129,7 @@ __device__ __forceinline__ Row row_of(const BiasedParams& p, const Chunk& c, int
   r.hi = pos + 1;
   if (p.prefix_lens) r.hi = max(r.hi, min(p.prefix_lens[b], c.ctx));
   r.hi = max(r.hi, r.lo);
-  r.pos = (float)pos;
+  r.pos = pos;
   r.slope = BIAS ? p.slopes[g * p.group + R % p.group] * kLog2e : 0.f;
   return r;
 }
@@ -224,7 +224,7 @@ struct Columns {
         a[r] = fmaf(raw[r], CAP ? cap_factor(p, raw[r]) : scale, off);
       }
     }
-    base = BIAS ? row.slope * ((float)(t0 + 4 * h) - row.pos) : CAP ? -neg : 0.f;
+    base = BIAS ? row.slope * (float)(t0 + 4 * h - row.pos) : CAP ? -neg : 0.f;
     return a;
   }
   __device__ __forceinline__ void reshape(const BiasedParams& p, floatx16_t& a, const floatx16_t& raw, int t0, bool edge,
@@ -237,7 +237,7 @@ struct Columns {
       }
     }
     if (BIAS && !linear) {
-      const float d0 = row.pos - (float)(t0 + 4 * h);
+      const float d0 = (float)(row.pos - t0 - 4 * h);
 #pragma unroll
       for (int r = 0; r < 16; ++r) a[r] = fmaf(2.f * row.slope, fminf(d0 - (float)(8 * (r >> 2) + (r & 3)), 0.f), a[r]);
     }

@@ -49,7 +49,7 @@ constexpr int kDecodeLdsBytes = (kWaves * 16 * D * 2 > (2 * kWaves * GP + kWaves
 template <int D, bool CAP, bool BIAS>
 __device__ __forceinline__ void decode_tile(const BiasedParams& p, WaveState<D>& S, KvTile<D>& T,
                                             const uint4 (&qb)[D / 32], lds_u8_t* stage, int t0, int lo, int hi,
-                                            bool edge, int q, int n, float lo_part, float scale, float pos, float slope) {
+                                            bool edge, int q, int n, float lo_part, float scale, int pos, float slope) {
   constexpr int VW = D / 32;
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
@@ -91,7 +91,7 @@ __device__ __forceinline__ void decode_tile(const BiasedParams& p, WaveState<D>&
     for (int r = 0; r < 4; ++r) e[r] = raw[r] * scale;
   }
   if constexpr (BIAS) {
-    const float d0 = pos - (float)(t0 + q);
+    const float d0 = (float)(pos - t0 - q);
 #pragma unroll
     for (int r = 0; r < 4; ++r) e[r] = fmaf(-slope, fabsf(d0 - (float)(4 * r)), e[r]);
   }
@@ -243,7 +243,7 @@ __device__ __forceinline__ void decode_body(const BiasedParams& p, int wg, lds_u
           ld += kWaves;
           const int t0 = (j0 + c0 + i) * 16;
           decode_tile<D, CAP, BIAS>(p, S, T[s], qb, stage, t0, lo, hi, t0 < lo || t0 + 16 > hi, q, n, lo_part, scale,
-                                    (float)(ctx - 1), slope);
+                                    ctx - 1, slope);
           i += kWaves;
           done = i >= cn;
         }
