@@ -165,7 +165,7 @@ int paged_attn_biased_workspace_size(const pa_kv_pool *pool, int32_t batch, int3
  * in the cache already) with these scores.
  *   pool             head_dim 64 or 128
  *   q, block_tables, bt_stride, context_lens, batch, scale, max_context_len
- *                    as in paged_attn_decode
+ *                    as in paged_attn_decode; max_context_len below 2^30
  *   num_q_heads      any multiple of the pool's num_kv_heads
  *   softcap          0 (none) or positive, finite (PA_EUNSUPPORTED where its
  *                    ratio to scale leaves the range of fp32)
@@ -184,7 +184,7 @@ int paged_attn_decode_biased(const pa_kv_pool *pool, const void *q, const int32_
 
 /* Attention of each sequence's chunk of new tokens (their K and V in the cache
  * already) with these scores; as paged_attn_extend, for head_dim 64 too, any
- * number of query heads per KV head and any context length.
+ * number of query heads per KV head and contexts below 2^30 tokens.
  *   q, q_start, total_q, block_tables, bt_stride, context_lens, batch, scale,
  *   max_context_len, max_chunk, out     as in paged_attn_extend; rows of out
  *                    behind the last sequence are left as they are

@@ -324,7 +324,9 @@ int plan_biased(const pa_kv_pool* pool, int32_t batch, int32_t num_q_heads, int3
   if (num_q_heads <= 0 || num_q_heads % pool->num_kv_heads != 0)
     return fail(PA_EINVAL, "%s: num_q_heads = %d is not a positive multiple of num_kv_heads = %d", fn, num_q_heads,
                 pool->num_kv_heads);
-  if (max_context_len < 0) return fail(PA_EINVAL, "%s: max_context_len = %d < 0", fn, max_context_len);
+  // the kernels' token indexes stay below the mark of a row that sees nothing, 2^30 - 1
+  if (max_context_len < 0 || max_context_len >= 1 << 30)
+    return fail(PA_EINVAL, "%s: max_context_len = %d outside [0, 2^30)", fn, max_context_len);
   if (max_chunk < 0 || max_chunk > std::max(max_context_len, 1))
     return fail(PA_EINVAL, "%s: max_chunk = %d outside [0, max_context_len = %d]", fn, max_chunk, max_context_len);
   if (window < 0) return fail(PA_EINVAL, "%s: window = %d < 0", fn, window);
