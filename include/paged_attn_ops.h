@@ -94,7 +94,7 @@ int pa_rope_destroy(pa_rope *rope);
  *   eps           >= 0, added to the mean square
  *   dtype         PA_BF16, PA_FP16 or PA_FP32
  *   positions     device int32 [tokens]
- *   tokens        >= 0 (0 is a no-op)
+ *   tokens        0 (a no-op) .. 2^26 - 64
  *   q_out, k_out  rows like q and k; each may be its input itself (same pointer
  *                 and stride), else they overlap no input */
 int paged_attn_norm_rope(const pa_rope *rope, const void *q, int64_t q_stride, int32_t num_q_heads,
@@ -117,7 +117,7 @@ int paged_attn_norm_rope(const pa_rope *rope, const void *q, int64_t q_stride, i
  *   q_start       device int32 [batch + 1], nondecreasing from 0: sequence b's
  *                 rows are q_start[b] .. q_start[b+1] - 1; or NULL: row b is
  *                 sequence b's single new token
- *   total_q       rows of q, k, v and q_out; rows behind the last sequence are
+ *   total_q       rows of q, k, v and q_out, 0 .. 2^26 - 64; rows behind the last sequence are
  *                 neither read into anything nor written
  *   block_tables  device int32 [batch][bt_stride]; the blocks of the new slots
  *                 must belong to sequence b alone (see paged_attn_append_kv)

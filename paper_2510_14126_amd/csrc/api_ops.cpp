@@ -24,6 +24,10 @@ struct pa_rope {
 namespace {
 using pa::fail;
 
+// A launch's threads are counted in 32 bits.
+constexpr int64_t kMostWorkgroups = 0xffffffffLL / 256;
+constexpr int32_t kMostTokens = (1 << 26) - 64;       // of the row operators: one wavefront per token at least
+
 constexpr double kTwoPi = 6.283185307179586476925286766559;
 
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
@@ -156,7 +160,8 @@ int paged_attn_norm_rope(const pa_rope* rope, const void* q, int64_t q_stride, i
   pa::RopeParams p{};
   int rc = rope_params(rope, num_q_heads, num_kv_heads, q_weight, k_weight, eps, dtype, &p, fn);
   if (rc) return rc;
-  if (tokens < 0) return fail(PA_EINVAL, "%s: tokens = %d < 0", fn, tokens);
+  if (tokens < 0 || tokens > kMostTokens)
+    return fail(PA_EINVAL, "%s: tokens = %d outside [0, 2^26 - 64]", fn, tokens);
   if (tokens == 0 || num_q_heads + num_kv_heads == 0) return PA_OK;
   const int64_t elem = type_bytes(dtype);
   const struct { const void* x; int64_t stride; int32_t heads; const char* name; } rows[] = {
@@ -196,7 +201,8 @@ int paged_attn_rope_append(const pa_kv_pool* pool, const pa_rope* rope, const vo
   if (rope->head_dim != pool->head_dim)
     return fail(PA_EINVAL, "%s: the rotation's head_dim = %d, the pool's %d", fn, rope->head_dim, pool->head_dim);
   if (batch < 0) return fail(PA_EINVAL, "%s: batch = %d < 0", fn, batch);
-  if (total_q < 0) return fail(PA_EINVAL, "%s: total_q = %d < 0", fn, total_q);
+  if (total_q < 0 || total_q > kMostTokens)
+    return fail(PA_EINVAL, "%s: total_q = %d outside [0, 2^26 - 64]", fn, total_q);
   if (bt_stride < 1 || (int64_t)bt_stride * PA_BLOCK_SIZE > 0x7fffffffLL)
     return fail(PA_EINVAL, "%s: bt_stride = %d outside [1, 2^27)", fn, bt_stride);
   if (batch == 0 || total_q == 0) return PA_OK;
@@ -368,6 +374,9 @@ int biased_impl(const pa_kv_pool* pool, const void* q, const int32_t* q_start, i
   if (!aligned(block_tables, 4) || !aligned(context_lens, 4) || !aligned(q_start, 4) || !aligned(slopes, 4) ||
       !aligned(first_tokens, 4) || !aligned(prefix_lens, 4))
     return fail(PA_EINVAL, "%s: an index, length or slope array is not 4-byte aligned", fn);
+  const int64_t row_tiles = (int64_t)batch * pl.tiles * pool->num_kv_heads;
+  if (row_tiles * pl.parts > kMostWorkgroups || (pl.parts > 1 && (row_tiles * pl.tile_rows + 3) / 4 > kMostWorkgroups))
+    return fail(PA_EINVAL, "%s: grid too large", fn);
   const size_t o_bytes = biased_part_o_bytes(pl, slots, pool->head_dim);
   const size_t need = o_bytes + biased_lse_bytes(pl, slots);
   if (workspace_bytes < need)
