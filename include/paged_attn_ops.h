@@ -68,7 +68,7 @@ int pa_rope_frequencies(int32_t rotary_dim, double base, int32_t scaling, double
  *   rotary_dim  a multiple of 16, 0 .. head_dim; 0: no rotation (norms alone)
  *   layout      PA_ROPE_HALF or PA_ROPE_INTERLEAVED
  *   freqs       [rotary_dim / 2] finite values, copied
- *   magnitude   finite; multiplies the rotated values
+ *   magnitude   finite in fp32; multiplies the rotated values
  *   out         receives the handle; untouched on error */
 typedef struct pa_rope pa_rope;
 int pa_rope_create(int32_t head_dim, int32_t rotary_dim, int32_t layout, const double *freqs,

@@ -135,7 +135,7 @@ int pa_rope_create(int32_t head_dim, int32_t rotary_dim, int32_t layout, const d
   if (rotary_dim > 0 && !freqs) return fail(PA_EINVAL, "%s: freqs is NULL", fn);
   for (int i = 0; i < rotary_dim / 2; ++i)
     if (!std::isfinite(freqs[i])) return fail(PA_EINVAL, "%s: freqs[%d] is not finite", fn, i);
-  if (!std::isfinite(magnitude)) return fail(PA_EINVAL, "%s: magnitude is not finite", fn);
+  if (!(std::fabs(magnitude) <= FLT_MAX)) return fail(PA_EINVAL, "%s: magnitude is not finite in fp32", fn);
   pa_rope* r = new (std::nothrow) pa_rope{};
   if (!r) return fail(PA_ENOMEM, "%s: host allocation failed", fn);
   r->head_dim = head_dim;

@@ -49,3 +49,10 @@ def test_biased_grids_beyond_the_threads_of_a_launch():
         with pytest.raises(pa.PagedAttnError) as e:
             call()
         assert e.value.code == pa.PA_EINVAL and "grid too large" in str(e.value)
+
+
+@pytest.mark.parametrize("magnitude", [1e39, -1e300])
+def test_magnitudes_beyond_fp32(magnitude):
+    with pytest.raises(pa.PagedAttnError) as e:
+        pa.pa_rope_create(64, 16, pa.PA_ROPE_HALF, [1.0] * 8, magnitude)
+    assert e.value.code == pa.PA_EINVAL and "magnitude" in str(e.value)
