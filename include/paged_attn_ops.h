@@ -147,10 +147,12 @@ int paged_attn_rope_append(const pa_kv_pool *pool, const pa_rope *rope, const vo
  * So first_tokens holds the start of each row's document in a sequence packed
  * from documents, window is a sliding window (the row's own token and the
  * window - 1 before it), and a prefix sees itself whole.  A row that sees
- * nothing gives zeros.  What hidden tokens hold (NaN and infinities too) has no
- * effect; an infinity or NaN that a row does see makes its outputs infinite or
- * NaN.  Weights reach the matrix cores to about 2^-17, as everywhere in this
- * library; sums are fp32.
+ * nothing gives zeros.  What hidden tokens hold (NaN and infinities too) changes
+ * no bit of a row.  An infinity or NaN in V that a row does see, a NaN among its
+ * scores, and +infinity there without a softcap (under one it is the cap) make
+ * its outputs infinite or NaN; a score of -infinity weighs nothing, and a row of
+ * those alone gives zeros.  Weights reach the matrix cores to about 2^-17, as
+ * everywhere in this library; sums are fp32.
  * ------------------------------------------------------------------------- */
 
 /* Bytes of the workspace of a biased decode (max_chunk 1) or extend: room for
