@@ -29,7 +29,13 @@ biased_decode_kernel(const BiasedParams p) {
   biased::decode_body<D, GP, CAP, BIAS, AUX>(p, blockIdx.x, (lds_u8_t*)smem);
 }
 
-// One row per workgroup, NW = 8 wavefronts on it, or four rows (NW = 1).
+// One row per workgroup, NW = 8 wavefronts on it, or four rows (NW = 1): eight
+// where a row has more partitions than one wavefront loads together and the rows
+// alone do not fill the GPU's wavefronts.  Whole decodes, one wavefront per row /
+// eight, capped: 64 rows of 32 partitions (a sequence of 30011 tokens, 64 heads over
+// 8) 27.3 / 25.1 us, 8 of 256 (100000 tokens, 8 over 1) 36.7 / 19.5; with at most eight
+// partitions, or more rows, the same or slower: 128 rows of 8 (four of 16384, 32 over
+// 8) 45.4 / 45.6, 1024 of 16 (sixteen of 32768, 64 over 8) 335.4 / 336.0.
 constexpr int kMergeWaves = 8;
 template <int D, int NW>
 __global__ void __launch_bounds__(64 * (NW > 1 ? NW : kWaves)) biased_merge_kernel(const BiasedParams p) {

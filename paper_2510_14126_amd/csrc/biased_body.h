@@ -374,7 +374,7 @@ struct Columns {
 // The order of a range's stages: with a distance bias from the nearest tokens to
 // the farthest, so that the running max is found first (upwards it rises with
 // every stage of a steep head, and each rise rescales the outputs: a prompt of
-// 8191 tokens upwards 858 us, downwards 726).  at(s): stage of step s (past the last step
+// 8191 tokens upwards 841 us, downwards 728).  at(s): stage of step s (past the last step
 // the last stage again); chunk(s): which 64 blocks hold it.
 template <bool DOWN>
 struct Walk {
@@ -696,8 +696,8 @@ __device__ __forceinline__ void split_body(const BiasedParams& p, int wg, lds_u8
 // its writing and precede its next writing.  Publishing first leaves scores and
 // weights in one run of instructions without a branch (masked stages have one
 // while they are published), exponentials between the MFMAs of the scores: scores
-// before it / after, 8191 tokens with slopes 774 / 759 us, 16 chunks of 600 over
-// 2904 capped 674 / 673, four of 3001..4096 tokens in documents of 61..1500 213 / 208.
+// before it / after, 8191 tokens with slopes 740 / 728 us, 16 chunks of 600 over
+// 2904 capped 733 / 727, four of 3001..4096 tokens in documents of 61..1500 206 / 205.
 // --------------------------------------------------------------------------
 constexpr int kSlots = 3;
 template <int D> constexpr int kBigRow = kSlots * kStageBytes<D>;         // one value per row, per wavefront
