@@ -208,8 +208,9 @@ struct Columns {
   //
   // reshape: in a stage with scores beyond the polynomial those alone anew, so that
   // no score's bits depend on another, which its row may not see; in one with
-  // tokens after a row's position (not linear) what |p - t| is more than p - t, twice
-  // t - p; then the masks, in a stage with hidden tokens (edge).
+  // tokens after a row's position (not linear) base and the FMA's part for |p - t|
+  // (small numbers both, as before: large ones would cost bits); then the masks, in a
+  // stage with hidden tokens (edge).
   __device__ __forceinline__ floatx16_t shape(const BiasedParams& p, const floatx16_t& raw, int t0, int h) {
     floatx16_t a = raw;
     if constexpr (CAP) {
@@ -238,8 +239,10 @@ struct Columns {
     }
     if (BIAS && !linear) {
       const float d0 = (float)(row.pos - t0 - 4 * h);
+      base = -row.slope * fabsf(d0);                       // of the lane's first token, before the row or after it
 #pragma unroll
-      for (int r = 0; r < 16; ++r) a[r] = fmaf(2.f * row.slope, fminf(d0 - (float)(8 * (r >> 2) + (r & 3)), 0.f), a[r]);
+      for (int r = 0; r < 16; ++r)
+        a[r] = fmaf(2.f * row.slope, fminf(fmaxf(d0, 0.f) - (float)(8 * (r >> 2) + (r & 3)), 0.f), a[r]);
     }
     if (edge) {
       // bit k: the row sees token t0 + 4h + k

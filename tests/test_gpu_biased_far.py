@@ -44,3 +44,17 @@ def test_far_positions(form, cap):
                                     c.scale, cap, t["slopes"], WINDOW, None, None, top, most, c.ws, size, out)
     torch.cuda.synchronize()
     assert (out.cpu().numpy().view(np.uint16) == near).all()
+
+
+@pytest.mark.parametrize("cap", [0.0, 30.0])
+@pytest.mark.parametrize("hq,hkv,d,chunks", [(4, 2, 128, [1500, 70]), (6, 2, 64, [1500]), (32, 8, 128, [700] * 3)])
+def test_rows_that_see_only_tokens_far_after_them(hq, hkv, d, chunks, cap):
+    """A prefix that sees itself whole and first tokens past the row: every distance is to a later token."""
+    print(f"[gpu case] far after {hq} {hkv} {d} {chunks} {cap}", flush=True)
+
+    def first(c, rng):
+        p = np.concatenate([np.arange(n) for n in c.ctx])
+        return np.minimum(p + 600, np.repeat(c.ctx, c.chunk) - 40)
+    c = Case(71, ctx=chunks, chunk=chunks, hq=hq, hkv=hkv, d=d, cap=cap, alibi=True, docs=first, prefix=chunks)
+    # a score's size is the bias of its row's nearest tokens too, at most slope * 1500
+    c.check(c.run(), None, 40.0 + 1500 * float(c.slopes.max()))
