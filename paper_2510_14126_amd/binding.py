@@ -2,8 +2,8 @@
 the functions a serving loop calls every step the native ``_pycall`` extension.
 
 Every function here has the name and argument order of the C function it
-calls; see ``include/paged_attn.h`` and ``include/paged_attn_ops.h`` for
-meanings, layouts and ownership.
+calls; see ``include/paged_attn.h``, ``include/paged_attn_ops.h`` and
+``include/paged_attn_tokens.h`` for meanings, layouts and ownership.
 Device buffers may be given as torch tensors (their ``data_ptr()`` is
 passed) or as raw integer addresses; ``stream`` is a HIP stream handle as an
 integer (for example ``torch.cuda.current_stream().cuda_stream``) or None
@@ -116,6 +116,27 @@ OPS_SIGNATURES = {
                                           _vp, _vp, _i32, _i32, _vp, _sz, _vp, _vp]),
 }
 
+# The same for paged_attn_tokens.h.
+PA_TREE_MAX_NODES = 256
+TOKENS_SIGNATURES = {
+    "paged_attn_tree_workspace_size": (_c_int, [_vp, _i32, _i32, _i32, _i32, ctypes.POINTER(_sz)]),
+    "paged_attn_extend_tree": (_c_int, [_vp, _vp, _vp, _i32, _vp, _vp, _i32, _vp, _i32, _i32, _f32, _f32, _i32, _i32,
+                                        _vp, _sz, _vp, _vp]),
+    "paged_attn_block_bounds": (_c_int, [_vp, _vp, _vp, _i32, _vp, _vp, _i32, _i32, _i32, _vp]),
+    "paged_attn_select_workspace_size": (_c_int, [_vp, _i32, _i32, _i32, ctypes.POINTER(_sz)]),
+    "paged_attn_select_blocks": (_c_int, [_vp, _vp, _vp, _vp, _i32, _vp, _i32, _i32, _i32, _i32, _i32, _i32, _vp, _sz,
+                                          _vp, _vp]),
+    "paged_attn_selected_workspace_size": (_c_int, [_vp, _i32, _i32, _i32, ctypes.POINTER(_sz)]),
+    "paged_attn_decode_selected": (_c_int, [_vp, _vp, _vp, _i32, _vp, _i32, _i32, _f32, _i32, _vp, _i32, _vp, _sz,
+                                            _vp, _vp]),
+    "paged_attn_weights_workspace_size": (_c_int, [_vp, _i32, _i32, _i32, ctypes.POINTER(_sz)]),
+    "paged_attn_decode_weights": (_c_int, [_vp, _vp, _vp, _i32, _vp, _i32, _i32, _f32, _i32, _f32, _vp, _vp, _i64, _vp,
+                                           _sz, _vp, _vp]),
+    "paged_attn_keep_heaviest": (_c_int, [_vp, _i64, _vp, _vp, _i32, _i32, _i32, _i32, _vp, _i32, _vp, _vp]),
+    "paged_attn_compact": (_c_int, [_vp, _vp, _i32, _vp, _i32, _vp, _vp, _i32, _i32, _vp, _i32, _vp, _vp, _vp, _i64,
+                                    _vp, _vp]),
+}
+
 
 class PagedAttnError(RuntimeError):
     def __init__(self, code: int, message: str):
@@ -134,7 +155,7 @@ def _load(path: str = LIB_PATH) -> ctypes.CDLL:
             f"{path} is missing: build the HIP library first "
             "(python -c 'import __graft_entry__ as g; g.build()')")
     lib = ctypes.CDLL(path)
-    for name, (res, args) in {**SIGNATURES, **OPS_SIGNATURES}.items():
+    for name, (res, args) in {**SIGNATURES, **OPS_SIGNATURES, **TOKENS_SIGNATURES}.items():
         fn = getattr(lib, name)
         fn.restype = res
         fn.argtypes = args
@@ -147,7 +168,10 @@ PER_STEP = ("paged_attn_decode", "paged_attn_decode_scheduled", "paged_attn_redu
             "paged_attn_decode_cascade_scheduled", "paged_attn_decode_cascade_groups", "paged_attn_reduce_cascade",
             "paged_attn_reduce_cascade_groups", "paged_attn_append_kv", "paged_attn_decode_append",
             "paged_attn_decode_cascade_append", "paged_attn_decode_noalloc", "paged_attn_extend",
-            "paged_attn_norm_rope", "paged_attn_rope_append", "paged_attn_decode_biased", "paged_attn_extend_biased")
+            "paged_attn_norm_rope", "paged_attn_rope_append", "paged_attn_decode_biased", "paged_attn_extend_biased",
+            "paged_attn_extend_tree", "paged_attn_block_bounds", "paged_attn_select_blocks",
+            "paged_attn_decode_selected", "paged_attn_decode_weights", "paged_attn_keep_heaviest",
+            "paged_attn_compact")
 
 
 def _ctypes_call(lib: ctypes.CDLL, name: str):
@@ -633,3 +657,77 @@ def paged_attn_extend_biased(pool: KVPool, q, q_start, total_q, block_tables, bt
                                             context_lens, batch, num_q_heads, scale, softcap, slopes, window,
                                             first_tokens, prefix_lens, max_context_len, max_chunk, workspace,
                                             workspace_bytes, out, stream))
+
+
+def _size(call, *args) -> int:
+    n = ctypes.c_size_t()
+    _check(call(*args, ctypes.byref(n)))
+    return n.value
+
+
+def paged_attn_tree_workspace_size(pool: KVPool, batch, num_q_heads, max_context_len, max_nodes) -> int:
+    return _size(_lib.paged_attn_tree_workspace_size, pool._handle(), batch, num_q_heads, max_context_len, max_nodes)
+
+
+def paged_attn_extend_tree(pool: KVPool, q, q_start, total_q, parents, block_tables, bt_stride, context_lens, batch,
+                           num_q_heads, scale, softcap, max_context_len, max_nodes, workspace, workspace_bytes, out,
+                           stream=None) -> None:
+    _check(_pycall.paged_attn_extend_tree(pool._handle(), q, q_start, total_q, parents, block_tables, bt_stride,
+                                          context_lens, batch, num_q_heads, scale, softcap, max_context_len, max_nodes,
+                                          workspace, workspace_bytes, out, stream))
+
+
+def paged_attn_block_bounds(pool: KVPool, bounds, block_tables, bt_stride, first_tokens, context_lens, batch,
+                            max_context_len, max_new, stream=None) -> None:
+    _check(_pycall.paged_attn_block_bounds(pool._handle(), bounds, block_tables, bt_stride, first_tokens, context_lens,
+                                           batch, max_context_len, max_new, stream))
+
+
+def paged_attn_select_workspace_size(pool: KVPool, batch, max_context_len, max_blocks) -> int:
+    return _size(_lib.paged_attn_select_workspace_size, pool._handle(), batch, max_context_len, max_blocks)
+
+
+def paged_attn_select_blocks(pool: KVPool, q, bounds, block_tables, bt_stride, context_lens, batch, num_q_heads,
+                             max_context_len, first_blocks, last_blocks, max_blocks, workspace, workspace_bytes,
+                             selected, stream=None) -> None:
+    _check(_pycall.paged_attn_select_blocks(pool._handle(), q, bounds, block_tables, bt_stride, context_lens, batch,
+                                            num_q_heads, max_context_len, first_blocks, last_blocks, max_blocks,
+                                            workspace, workspace_bytes, selected, stream))
+
+
+def paged_attn_selected_workspace_size(pool: KVPool, batch, num_q_heads, max_blocks) -> int:
+    return _size(_lib.paged_attn_selected_workspace_size, pool._handle(), batch, num_q_heads, max_blocks)
+
+
+def paged_attn_decode_selected(pool: KVPool, q, block_tables, bt_stride, context_lens, batch, num_q_heads, scale,
+                               max_context_len, selected, max_blocks, workspace, workspace_bytes, out,
+                               stream=None) -> None:
+    _check(_pycall.paged_attn_decode_selected(pool._handle(), q, block_tables, bt_stride, context_lens, batch,
+                                              num_q_heads, scale, max_context_len, selected, max_blocks, workspace,
+                                              workspace_bytes, out, stream))
+
+
+def paged_attn_weights_workspace_size(pool: KVPool, batch, num_q_heads, max_context_len) -> int:
+    return _size(_lib.paged_attn_weights_workspace_size, pool._handle(), batch, num_q_heads, max_context_len)
+
+
+def paged_attn_decode_weights(pool: KVPool, q, block_tables, bt_stride, context_lens, batch, num_q_heads, scale,
+                              max_context_len, decay, totals, totals_out, totals_stride, workspace, workspace_bytes,
+                              out, stream=None) -> None:
+    _check(_pycall.paged_attn_decode_weights(pool._handle(), q, block_tables, bt_stride, context_lens, batch,
+                                             num_q_heads, scale, max_context_len, decay, totals, totals_out,
+                                             totals_stride, workspace, workspace_bytes, out, stream))
+
+
+def paged_attn_keep_heaviest(totals, totals_stride, first_tokens, context_lens, batch, max_context_len, recent, keep,
+                             kept, kept_stride, kept_lens, stream=None) -> None:
+    _check(_pycall.paged_attn_keep_heaviest(totals, totals_stride, first_tokens, context_lens, batch, max_context_len,
+                                            recent, keep, kept, kept_stride, kept_lens, stream))
+
+
+def paged_attn_compact(pool: KVPool, block_tables, bt_stride, dst_tables, dst_stride, first_tokens, context_lens, batch,
+                       max_context_len, kept, kept_stride, kept_lens, totals, totals_out, totals_stride, new_lens,
+                       stream=None) -> None:
+    _check(_pycall.paged_attn_compact(pool._handle(), block_tables, bt_stride, dst_tables, dst_stride, first_tokens,
+                                      context_lens, batch, max_context_len, kept, kept_stride, kept_lens, totals,
+                                      totals_out, totals_stride, new_lens, stream))

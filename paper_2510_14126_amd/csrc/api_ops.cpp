@@ -350,11 +350,28 @@ int plan_biased(const pa_kv_pool* pool, int32_t batch, int32_t num_q_heads, int3
   return PA_OK;
 }
 
-int biased_impl(const pa_kv_pool* pool, const void* q, const int32_t* q_start, int32_t total_q,
+}  // namespace
+
+}  // extern "C"
+
+namespace pa {
+
+int biased_size(const pa_kv_pool* pool, int32_t batch, int32_t num_q_heads, int32_t max_context_len,
+                int32_t max_chunk, int32_t window, size_t* bytes_out, const char* fn) {
+  if (!bytes_out) return fail(PA_EINVAL, "%s: NULL output pointer", fn);
+  BiasedPlan pl;
+  int64_t slots = 0;
+  const int rc = plan_biased(pool, batch, num_q_heads, max_context_len, max_chunk, window, 0, &pl, &slots, fn);
+  if (rc) return rc;
+  *bytes_out = biased_part_o_bytes(pl, slots, pool->head_dim) + biased_lse_bytes(pl, slots);
+  return PA_OK;
+}
+
+int biased_call(const pa_kv_pool* pool, const void* q, const int32_t* q_start, int32_t total_q, const int32_t* parents,
                 const int32_t* block_tables, int32_t bt_stride, const int32_t* context_lens, int32_t batch,
                 int32_t num_q_heads, float scale, float softcap, const float* slopes, int32_t window,
                 const int32_t* first_tokens, const int32_t* prefix_lens, int32_t max_context_len, int32_t max_chunk,
-                void* workspace, size_t workspace_bytes, void* out, void* stream, const char* fn) {
+                void* workspace, size_t workspace_bytes, void* out, void* stream, BiasedLaunch launch, const char* fn) {
   pa::BiasedPlan pl;
   int64_t slots = 0;
   int rc = plan_biased(pool, batch, num_q_heads, max_context_len, max_chunk, window, total_q, &pl, &slots, fn);
@@ -372,7 +389,7 @@ int biased_impl(const pa_kv_pool* pool, const void* q, const int32_t* q_start, i
     return fail(PA_EINVAL, "%s: q, block_tables, context_lens and out must be non-NULL", fn);
   if (!aligned(q, 16) || !aligned(out, 16)) return fail(PA_EINVAL, "%s: q/out are not 16-byte aligned", fn);
   if (!aligned(block_tables, 4) || !aligned(context_lens, 4) || !aligned(q_start, 4) || !aligned(slopes, 4) ||
-      !aligned(first_tokens, 4) || !aligned(prefix_lens, 4))
+      !aligned(first_tokens, 4) || !aligned(prefix_lens, 4) || !aligned(parents, 4))
     return fail(PA_EINVAL, "%s: an index, length or slope array is not 4-byte aligned", fn);
   const int64_t row_tiles = (int64_t)batch * pl.tiles * pool->num_kv_heads;
   if (row_tiles * pl.parts > kMostWorkgroups || (pl.parts > 1 && (row_tiles * pl.tile_rows + 3) / 4 > kMostWorkgroups))
@@ -393,6 +410,7 @@ int biased_impl(const pa_kv_pool* pool, const void* q, const int32_t* q_start, i
   p.slopes = slopes;
   p.first_tokens = first_tokens;
   p.prefix_lens = prefix_lens;
+  p.parents = parents;
   p.out = static_cast<uint16_t*>(out);
   p.part_o = static_cast<float*>(workspace);
   p.part_lse = need > 0 ? reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + o_bytes) : nullptr;
@@ -439,23 +457,19 @@ int biased_impl(const pa_kv_pool* pool, const void* q, const int32_t* q_start, i
         !std::isfinite(p.two_z) || (s > 0.0 && reach / z > kMostRaw))
       return fail(PA_EUNSUPPORTED, "%s: softcap = %g with scale = %g leaves the range of fp32", fn, softcap, scale);
   }
-  const hipError_t e = pa::launch_biased(p, static_cast<hipStream_t>(stream));
+  const hipError_t e = launch(p, static_cast<hipStream_t>(stream));
   if (e != hipSuccess) return fail(PA_EHIP, "%s: kernel launch failed: %s", fn, hipGetErrorString(e));
   return PA_OK;
 }
 
-}  // namespace
+}  // namespace pa
+
+extern "C" {
 
 int paged_attn_biased_workspace_size(const pa_kv_pool* pool, int32_t batch, int32_t num_q_heads,
                                      int32_t max_context_len, int32_t max_chunk, int32_t window, size_t* bytes_out) {
-  const char* fn = "paged_attn_biased_workspace_size";
-  if (!bytes_out) return fail(PA_EINVAL, "%s: NULL output pointer", fn);
-  pa::BiasedPlan pl;
-  int64_t slots = 0;
-  const int rc = plan_biased(pool, batch, num_q_heads, max_context_len, max_chunk, window, 0, &pl, &slots, fn);
-  if (rc) return rc;
-  *bytes_out = biased_part_o_bytes(pl, slots, pool->head_dim) + biased_lse_bytes(pl, slots);
-  return PA_OK;
+  return pa::biased_size(pool, batch, num_q_heads, max_context_len, max_chunk, window, bytes_out,
+                         "paged_attn_biased_workspace_size");
 }
 
 int paged_attn_decode_biased(const pa_kv_pool* pool, const void* q, const int32_t* block_tables, int32_t bt_stride,
@@ -463,9 +477,9 @@ int paged_attn_decode_biased(const pa_kv_pool* pool, const void* q, const int32_
                              float softcap, const float* slopes, int32_t window, const int32_t* first_tokens,
                              int32_t max_context_len, void* workspace, size_t workspace_bytes, void* out,
                              void* stream) {
-  return biased_impl(pool, q, nullptr, batch, block_tables, bt_stride, context_lens, batch, num_q_heads, scale,
-                     softcap, slopes, window, first_tokens, nullptr, max_context_len, 1, workspace, workspace_bytes,
-                     out, stream, "paged_attn_decode_biased");
+  return pa::biased_call(pool, q, nullptr, batch, nullptr, block_tables, bt_stride, context_lens, batch, num_q_heads,
+                         scale, softcap, slopes, window, first_tokens, nullptr, max_context_len, 1, workspace,
+                         workspace_bytes, out, stream, pa::launch_biased, "paged_attn_decode_biased");
 }
 
 int paged_attn_extend_biased(const pa_kv_pool* pool, const void* q, const int32_t* q_start, int32_t total_q,
@@ -476,9 +490,9 @@ int paged_attn_extend_biased(const pa_kv_pool* pool, const void* q, const int32_
                              void* out, void* stream) {
   const char* fn = "paged_attn_extend_biased";
   if (batch > 0 && total_q > 0 && max_chunk > 0 && !q_start) return fail(PA_EINVAL, "%s: q_start is NULL", fn);
-  return biased_impl(pool, q, q_start, total_q, block_tables, bt_stride, context_lens, batch, num_q_heads, scale,
-                     softcap, slopes, window, first_tokens, prefix_lens, max_context_len, max_chunk, workspace,
-                     workspace_bytes, out, stream, fn);
+  return pa::biased_call(pool, q, q_start, total_q, nullptr, block_tables, bt_stride, context_lens, batch, num_q_heads,
+                         scale, softcap, slopes, window, first_tokens, prefix_lens, max_context_len, max_chunk,
+                         workspace, workspace_bytes, out, stream, pa::launch_biased, fn);
 }
 
 }  // extern "C"

@@ -56,6 +56,7 @@ using mfma::lds_u32x4_t;
 using mfma::pack_bf16;
 using mfma::u32x4_t;
 typedef __attribute__((address_space(3))) uint16_t lds_u16_t;
+typedef __attribute__((address_space(3))) uint32_t lds_u32_t;
 
 constexpr int kTokens = 32;                                 // per stage: two blocks
 template <int D> constexpr int kStageBytes = 2 * kTokens * D * 2;   // K rows, then V rows
@@ -150,11 +151,61 @@ __device__ __forceinline__ float cap_any(const BiasedParams& p, float x) {
   return cap_is_near(p, x) ? cap_near(p, x) : z;
 }
 
+// Trees (TREE): a row sees the tokens before the chunk, and of the chunk the node's
+// ancestors and itself: bit j of the row's kTreeWords words in LDS is node j (a word
+// of zeros behind them takes the reads past the last node).  Rows are kTreePitch
+// words apart: 32 lanes that read one word of 32 rows touch 32 banks.
+constexpr int kTreeWords = kTreeMostNodes / 32;
+constexpr int kTreePitch = kTreeWords + 1;
+template <int ROWS> constexpr int kTreeBytes = ROWS * kTreePitch * 4;
+
+// Fills the words of the workgroup's ROWS rows from row0 on and ends with a
+// barrier.  The parents go through LDS (up: 2 kTreeMostNodes bytes that nobody reads
+// yet), for a path is a chain of dependent reads.
+template <int ROWS>
+__device__ __forceinline__ void tree_rows(const BiasedParams& p, const Chunk& c, int row0, lds_u32_t* words, lds_u16_t* up) {
+  constexpr int kNone = 0xffff;
+  for (int j = threadIdx.x; j < c.len; j += 64 * kWaves) {          // c.len <= max_chunk <= kTreeMostNodes
+    const int x = p.parents[c.start + j];
+    up[j] = (uint16_t)(x >= 0 && x < j ? x : kNone);
+  }
+  __syncthreads();
+  if (threadIdx.x < ROWS) {
+    const int R = row0 + threadIdx.x;
+    int j = R < c.len * p.group ? R / p.group : kNone;
+    lds_u32_t* row = words + threadIdx.x * kTreePitch;
+    row[kTreeWords] = 0u;
+#pragma unroll 1
+    for (int w = kTreeWords - 1; w >= 0; --w) {
+      uint32_t bits = 0u;
+      while (j != kNone && j >= 32 * w) {                           // nodes descend
+        bits |= 1u << (j & 31);
+        j = up[j];
+      }
+      row[w] = bits;
+    }
+  }
+  __syncthreads();
+}
+
+// Bits of a row's nodes from `from` on (k: node from + k); the context before the
+// chunk (from + k < 0) is seen.
+__device__ __forceinline__ uint32_t tree_bits(const lds_u32_t* row, int from) {
+  const int w = min(max(from, 0) >> 5, kTreeWords);
+  const uint32_t a = row[w], b = row[min(w + 1, kTreeWords)];
+  const int s = max(from, 0) & 31;
+  const uint32_t x = s == 0 ? a : (a >> s) | (b << (32 - s));
+  if (from <= -32) return 0xffffffffu;
+  return from < 0 ? (x << -from) | (0xffffffffu >> (32 + from)) : x;
+}
+
 // The 32 columns of one wavefront: queries (Q^T operand of step s: dims 16s + 8h
 // .. of column n), softmax state, outputs.
-template <int D, bool CAP, bool BIAS>
+template <int D, bool CAP, bool BIAS, bool TREE = false>
 struct Columns {
   Row row;
+  const lds_u32_t* tree;        // TREE: the words of the wavefront's first row
+  int drafted;                  // TREE: the chunk's first token
   float m, neg, l;              // running max, -m (0 while it is -inf), the lane's share of the sum
   floatx16_t o[D / 32];         // [j][r]: row 8(r/4) + 4h + r%4, dim 32j + n
   float scale;                  // |scale_log2|
@@ -247,7 +298,8 @@ struct Columns {
     if (edge) {
       // bit k: the row sees token t0 + 4h + k
       const int from = max(row.lo - (t0 + 4 * h), 0), to = min(row.hi - (t0 + 4 * h), 32);
-      const uint32_t seen = to > from ? (0xffffffffu >> (32 - (to - from))) << from : 0u;
+      uint32_t seen = to > from ? (0xffffffffu >> (32 - (to - from))) << from : 0u;
+      if constexpr (TREE) seen &= tree_bits(tree + ((int)threadIdx.x & 31) * kTreePitch, t0 + 4 * h - drafted);
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const uint32_t keep = (uint32_t)__builtin_amdgcn_sbfe((int)seen, 8 * (r >> 2) + (r & 3), 1);
@@ -368,7 +420,9 @@ struct Columns {
         const float y = (x & 0x7f80u) == 0x7f80u ? bf16_lo(x) : 0.f;
 #pragma unroll
         for (int r = 0; r < 16; ++r)
-          if (t0 + t >= __float_as_int(from[r]) && t0 + t < __float_as_int(to[r])) o[j][r] += y;
+          if (t0 + t >= __float_as_int(from[r]) && t0 + t < __float_as_int(to[r]) &&
+              (!TREE || (tree_bits(tree + (8 * (r >> 2) + 4 * h + (r & 3)) * kTreePitch, t0 + t - drafted) & 1u) != 0))
+            o[j][r] += y;
       }
     }
   }
@@ -456,8 +510,10 @@ static_assert(kWaves * (kWaves - 1) * kSwapBytes<64> <= kSplitStats<64>, "the me
 constexpr float kWhole = __builtin_inff();
 
 // AUX: cache policy of the tiles' loads.
-template <int D, bool CAP, bool BIAS, int AUX>
+// TREE: kTreeBytes<kBiasedTileRows> of LDS follow kSplitLdsBytes.
+template <int D, bool CAP, bool BIAS, int AUX, bool TREE = false>
 __device__ __forceinline__ void split_body(const BiasedParams& p, int wg, lds_u8_t* smem) {
+  using Cols = Columns<D, CAP, BIAS, TREE>;
   constexpr int kRows = kBiasedTileRows;
   const int lane = threadIdx.x & 63;
   const int wave = wave_uniform(threadIdx.x >> 6);
@@ -496,14 +552,14 @@ __device__ __forceinline__ void split_body(const BiasedParams& p, int wg, lds_u8
   {
     const uint16_t* q_row = p.q + ((size_t)(c.start + R / p.group) * p.num_q_heads + g * p.group + R % p.group) * D;
 #pragma unroll
-    for (int i = 0; i < D / 64; ++i) q_mine[i] = Columns<D, CAP, BIAS>::query(p, q_row, wave * (D / 64) + i, h);
+    for (int i = 0; i < D / 64; ++i) q_mine[i] = Cols::query(p, q_row, wave * (D / 64) + i, h);
   }
   const Row row = row_of<BIAS>(p, c, b, g, R);
   const bool none = row.hi <= row.lo;
   const int lo = min32(none ? 0x3fffffff : row.lo);     // tokens that some row sees
   const int hi = max32(none ? 0 : row.hi);
   const int all_lo = max32(row.lo);                     // tokens that every row sees
-  const int all_hi = min32(none ? 0 : row.hi);
+  const int all_hi = TREE ? c.first : min32(none ? 0 : row.hi);
 
   const int from_pos = c.first + row0 / p.group;        // position of the tile's first row
   // This partition's blocks.
@@ -519,8 +575,14 @@ __device__ __forceinline__ void split_body(const BiasedParams& p, int wg, lds_u8
     return;
   }
 
-  Columns<D, CAP, BIAS> C;
+  Cols C;
   C.init(p, row);
+  if constexpr (TREE) {
+    lds_u32_t* words = reinterpret_cast<lds_u32_t*>(smem + kSplitLdsBytes<D>);
+    tree_rows<kRows>(p, c, row0, words, reinterpret_cast<lds_u16_t*>(smem));
+    C.tree = words;
+    C.drafted = c.first;
+  }
   // The queries stay in LDS (all wavefronts have the same rows): in registers
   // they would not fit beside a stage in flight.
   lds_u32x4_t* ql = reinterpret_cast<lds_u32x4_t*>(smem + kSplitQuery<D>) + lane;
@@ -641,7 +703,7 @@ __device__ __forceinline__ void split_body(const BiasedParams& p, int wg, lds_u8
   if (p.parts > 1 && wave == 0 && lane < p.tile_rows)
     p.part_lse[slot * p.tile_rows + lane] = !split ? kWhole : (lt == 0.f ? -__builtin_inff() : mref + log2f(lt));
   float f[16];
-  Columns<D, CAP, BIAS>::per_row(rowv, h, n, fast_exp2(C.m - mref) * inv, f);
+  Cols::per_row(rowv, h, n, fast_exp2(C.m - mref) * inv, f);
   constexpr int kJ = D / 32;
   auto at = [&](int dst, int src) {   // outputs of wavefront src for wavefront dst
     return reinterpret_cast<lds_f32_t*>(smem + (dst * (kWaves - 1) + (src > dst ? src - 1 : src)) * kSwapBytes<D>) +
@@ -768,8 +830,10 @@ __device__ __forceinline__ bool ranked_tile(const BiasedParams& p, int i, int& b
   return true;
 }
 
-template <int D, bool CAP, bool BIAS>
+// TREE: kTreeBytes<kBiasedWgRows> of LDS follow kBigLdsBytes.
+template <int D, bool CAP, bool BIAS, bool TREE = false>
 __device__ __forceinline__ void big_body(const BiasedParams& p, int wg, lds_u8_t* smem) {
+  using Cols = Columns<D, CAP, BIAS, TREE>;
   const int lane = threadIdx.x & 63;
   const int wave = wave_uniform(threadIdx.x >> 6);
   const int h = lane >> 5;
@@ -796,7 +860,7 @@ __device__ __forceinline__ void big_body(const BiasedParams& p, int wg, lds_u8_t
   {
     const uint16_t* q_row = p.q + ((size_t)(c.start + R / p.group) * p.num_q_heads + g * p.group + R % p.group) * D;
 #pragma unroll
-    for (int s = 0; s < D / 16; ++s) q[s] = Columns<D, CAP, BIAS>::query(p, q_row, s, h);
+    for (int s = 0; s < D / 16; ++s) q[s] = Cols::query(p, q_row, s, h);
   }
   const Row row = row_of<BIAS>(p, c, b, g, R);
   int lo, hi, all_lo, all_hi;                          // tokens that some row, that every row of the workgroup sees
@@ -818,15 +882,21 @@ __device__ __forceinline__ void big_body(const BiasedParams& p, int wg, lds_u8_t
     lo = -y[0];
     hi = y[1];
     all_lo = y[2];
-    all_hi = -y[3];
+    all_hi = TREE ? c.first : -y[3];
     __syncthreads();                                   // `range` is used again
   }
   const int from_pos = c.first + tile * kBiasedWgRows / p.group;   // position of the workgroup's first row
   const int j0 = lo >> 4;
   const int cnt = hi > lo ? ((hi + 15) >> 4) - j0 : 0;
 
-  Columns<D, CAP, BIAS> C;
+  Cols C;
   C.init(p, row);
+  if constexpr (TREE) {
+    lds_u32_t* words = reinterpret_cast<lds_u32_t*>(smem + kBigLdsBytes<D>);
+    tree_rows<kBiasedWgRows>(p, c, tile * kBiasedWgRows, words, reinterpret_cast<lds_u16_t*>(smem));
+    C.tree = words + wave * kBiasedTileRows * kTreePitch;
+    C.drafted = c.first;
+  }
   auto query = [&](int s) { return q[s]; };
 
   constexpr size_t kTile = 16 * D;
@@ -941,7 +1011,7 @@ __device__ __forceinline__ void big_body(const BiasedParams& p, int wg, lds_u8_t
   swap32(lx, ly);
   const float lcol = lx + ly;
   float inv[16];
-  Columns<D, CAP, BIAS>::per_row(rowv, h, n, lcol == 0.f ? 0.f : 1.0f / lcol, inv);
+  Cols::per_row(rowv, h, n, lcol == 0.f ? 0.f : 1.0f / lcol, inv);
   lds_u8_t* out = smem + wave * (kBiasedTileRows * D * 2);
 #pragma unroll
   for (int r = 0; r < 16; ++r)

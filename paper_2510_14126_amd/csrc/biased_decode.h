@@ -45,11 +45,16 @@ constexpr int kDecodeLdsBytes = (kWaves * 16 * D * 2 > (2 * kWaves * GP + kWaves
                                     ? kWaves * 16 * D * 2 : (2 * kWaves * GP + kWaves * GP * D) * 4;
 
 // One block.  t0: its first token; tokens lo <= t < hi are seen, all 16 unless
-// `edge`; lo_part: 1 in the columns that carry the low parts, else 0.
-template <int D, bool CAP, bool BIAS>
+// `edge`; lo_part: 1 in the columns that carry the low parts, else 0.  keep(e): is
+// given the block's scores in log2 units, register r that of token t0 + 4r + q.
+struct KeepNone {
+  __device__ __forceinline__ void operator()(const float (&)[4]) const {}
+};
+template <int D, bool CAP, bool BIAS, typename Keep = KeepNone>
 __device__ __forceinline__ void decode_tile(const BiasedParams& p, WaveState<D>& S, KvTile<D>& T,
                                             const uint4 (&qb)[D / 32], lds_u8_t* stage, int t0, int lo, int hi,
-                                            bool edge, int q, int n, float lo_part, float scale, int pos, float slope) {
+                                            bool edge, int q, int n, float lo_part, float scale, int pos, float slope,
+                                            const Keep& keep = Keep()) {
   constexpr int VW = D / 32;
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
@@ -107,6 +112,8 @@ __device__ __forceinline__ void decode_tile(const BiasedParams& p, WaveState<D>&
     }
   }
 
+  keep(e);
+
   const float xmax = fmaxf(fmaxf(e[0], e[1]), fmaxf(e[2], e[3]));
   if (__builtin_amdgcn_ballot_w64(xmax > S.m + kLazyRescale) != 0) {
     const float bm = group_max4(xmax);
@@ -141,6 +148,74 @@ __device__ __forceinline__ void decode_tile(const BiasedParams& p, WaveState<D>&
     const uint32_t b1 = __builtin_amdgcn_perm(T.v[3][j >> 1], T.v[2][j >> 1], sel);
     S.o[j] = __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(pw, __builtin_bit_cast(short4_t, make_uint2(b0, b1)),
                                                        S.o[j], 0, 0, 0);
+  }
+}
+
+// The wavefronts' states become the rows' results: the low parts' output rows (GP ..
+// 2GP-1) are added to the high parts' (0 .. GP-1), then the wavefronts are merged
+// through LDS, as in the plain decode.  store(r, d, o0, o1, lt, mref): dims d and d+1
+// of row r < rows, normalised; lt: the sum of its weights 2^(e - mref), 0 where it saw
+// nothing.
+template <int D, int GP, typename Store>
+__device__ __forceinline__ void decode_merge(const WaveState<D>& S, lds_u8_t* smem, int wave, int q, int n, int rows,
+                                             const Store& store) {
+  constexpr int DPL = D / 16;   // dims per lane and token row
+  const float lrow = group_sum4(S.l);
+  floatx4_t sum[DPL / 2];
+#pragma unroll
+  for (int j = 0; j < DPL / 2; ++j)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      float x = S.o[j][r], y = S.o[j + DPL / 2][r];
+      if constexpr (GP == 8) swap32(x, y); else swap16(x, y);
+      sum[j][r] = x + y;
+    }
+  const int half = GP == 8 ? q >> 1 : q & 1;          // which half of the lane's dims
+  const int qrow = GP == 8 ? q & 1 : q >> 1;          // merge rows 4 * qrow + r
+  const bool keeps = GP == 8 || q < 2;                // else groups 2 and 3 hold copies
+  __syncthreads();
+  lds_f32_t* sm = reinterpret_cast<lds_f32_t*>(smem);       // [kWaves][GP]
+  lds_f32_t* sl = sm + kWaves * GP;                          // [kWaves][GP]
+  lds_f32_t* sacc = sl + kWaves * GP;                        // [kWaves][GP][D]
+  if (q == 0 && n < GP) {
+    sm[wave * GP + n] = S.m;
+    sl[wave * GP + n] = lrow;
+  }
+  if (keeps) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      lds_f32_t* row = sacc + (wave * GP + 4 * qrow + r) * D + DPL * n + (DPL / 2) * half;
+      if constexpr (D == 128) {
+        *reinterpret_cast<lds_floatx4_t*>(row) = floatx4_t{sum[0][r], sum[1][r], sum[2][r], sum[3][r]};
+      } else {
+        row[0] = sum[0][r];
+        row[1] = sum[1][r];
+      }
+    }
+  }
+  __syncthreads();
+  constexpr int kRowThreads = D / 2;                  // two output dims of a row per thread
+  constexpr int kRowsPerPass = 64 * kWaves / kRowThreads;
+  const int d = 2 * (threadIdx.x % kRowThreads);
+#pragma unroll
+  for (int r0 = 0; r0 < GP; r0 += kRowsPerPass) {
+    const int r = r0 + threadIdx.x / kRowThreads;
+    if (r >= rows) return;
+    float mx = sm[r];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) mx = fmaxf(mx, sm[w * GP + r]);
+    const float mref = mx == -__builtin_inff() ? 0.f : mx;
+    float lt = 0.f, o0 = 0.f, o1 = 0.f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float f = fast_exp2(sm[w * GP + r] - mref);
+      lt = fmaf(sl[w * GP + r], f, lt);
+      const floatx2_t a = *reinterpret_cast<const lds_floatx2_t*>(sacc + (w * GP + r) * D + d);
+      o0 = fmaf(a[0], f, o0);
+      o1 = fmaf(a[1], f, o1);
+    }
+    const float inv = lt == 0.f ? 0.f : 1.0f / lt;
+    store(r, d, o0 * inv, o1 * inv, lt, mref);
   }
 }
 
@@ -251,72 +326,16 @@ __device__ __forceinline__ void decode_body(const BiasedParams& p, int wg, lds_u
     }
   }
 
-  // Add the low parts' output rows (GP .. 2GP-1) to the high parts' (0 ..
-  // GP-1), then merge the wavefronts through LDS, as the plain decode does.
-  const float lrow = group_sum4(S.l);
-  floatx4_t sum[DPL / 2];
-#pragma unroll
-  for (int j = 0; j < DPL / 2; ++j)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      float x = S.o[j][r], y = S.o[j + DPL / 2][r];
-      if constexpr (GP == 8) swap32(x, y); else swap16(x, y);
-      sum[j][r] = x + y;
-    }
-  const int half = GP == 8 ? q >> 1 : q & 1;          // which half of the lane's dims
-  const int qrow = GP == 8 ? q & 1 : q >> 1;          // merge rows 4 * qrow + r
-  const bool keeps = GP == 8 || q < 2;                // else groups 2 and 3 hold copies
-  __syncthreads();
-  lds_f32_t* sm = reinterpret_cast<lds_f32_t*>(smem);       // [kWaves][GP]
-  lds_f32_t* sl = sm + kWaves * GP;                          // [kWaves][GP]
-  lds_f32_t* sacc = sl + kWaves * GP;                        // [kWaves][GP][D]
-  if (q == 0 && n < GP) {
-    sm[wave * GP + n] = S.m;
-    sl[wave * GP + n] = lrow;
-  }
-  if (keeps) {
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      lds_f32_t* row = sacc + (wave * GP + 4 * qrow + r) * D + DPL * n + (DPL / 2) * half;
-      if constexpr (D == 128) {
-        *reinterpret_cast<lds_floatx4_t*>(row) = floatx4_t{sum[0][r], sum[1][r], sum[2][r], sum[3][r]};
-      } else {
-        row[0] = sum[0][r];
-        row[1] = sum[1][r];
-      }
-    }
-  }
-  __syncthreads();
-  constexpr int kRowThreads = D / 2;                  // two output dims of a row per thread
-  constexpr int kRowsPerPass = 64 * kWaves / kRowThreads;
-  const int d = 2 * (threadIdx.x % kRowThreads);
-#pragma unroll
-  for (int r0 = 0; r0 < GP; r0 += kRowsPerPass) {
-    const int r = r0 + threadIdx.x / kRowThreads;
-    if (r >= p.group) return;
-    float mx = sm[r];
-#pragma unroll
-    for (int w = 1; w < kWaves; ++w) mx = fmaxf(mx, sm[w * GP + r]);
-    const float mref = mx == -__builtin_inff() ? 0.f : mx;
-    float lt = 0.f, o0 = 0.f, o1 = 0.f;
-#pragma unroll
-    for (int w = 0; w < kWaves; ++w) {
-      const float f = fast_exp2(sm[w * GP + r] - mref);
-      lt = fmaf(sl[w * GP + r], f, lt);
-      const floatx2_t a = *reinterpret_cast<const lds_floatx2_t*>(sacc + (w * GP + r) * D + d);
-      o0 = fmaf(a[0], f, o0);
-      o1 = fmaf(a[1], f, o1);
-    }
-    const float inv = lt == 0.f ? 0.f : 1.0f / lt;
+  decode_merge<D, GP>(S, smem, wave, q, n, p.group, [&](int r, int d, float o0, float o1, float lt, float mref) {
     if (split) {
-      store_partial2(p.part_o + (slot * p.tile_rows + r) * D + d, o0 * inv, o1 * inv);
+      store_partial2(p.part_o + (slot * p.tile_rows + r) * D + d, o0, o1);
       if (d == 0) p.part_lse[slot * p.tile_rows + r] = lt == 0.f ? -__builtin_inff() : mref + log2f(lt);
     } else {
       const size_t row = (size_t)b * p.num_q_heads + head0 + r;
-      *reinterpret_cast<uint32_t*>(p.out + row * D + d) = pack_bf16(o0 * inv, o1 * inv);
+      *reinterpret_cast<uint32_t*>(p.out + row * D + d) = pack_bf16(o0, o1);
       if (d == 0 && p.parts > 1) p.part_lse[slot * p.tile_rows + r] = kWhole;
     }
-  }
+  });
 }
 
 }  // namespace biased

@@ -1,0 +1,146 @@
+// The tokens that stay in a cache, and their move to the front of their sequences
+// (gfx950).
+#include "choose_body.h"
+#include "tokens.h"
+
+namespace pa {
+namespace {
+
+__device__ __forceinline__ int clamped(int x, int most) { return x < 0 ? 0 : (x > most ? most : x); }
+
+// ---- choice ----------------------------------------------------------------
+// One workgroup per sequence: the totals come from memory once, then from L2 once
+// per digit of the threshold.
+__global__ void __launch_bounds__(choose::kThreads) keep_kernel(const KeepParams p) {
+  __shared__ choose::Scratch scratch;
+  const int b = blockIdx.x;
+  const int ctx = clamped(p.context_lens[b], p.max_ctx);
+  const int first = p.first_tokens ? clamped(p.first_tokens[b], ctx) : 0;
+  const int recent = min(p.recent, ctx - first);
+  const int n = ctx - first - recent;                                   // candidates
+  const int want = min(max(p.keep - first - recent, 0), n);
+  int32_t* out = p.kept + (size_t)b * p.kept_stride;
+  for (int i = threadIdx.x; i < recent; i += choose::kThreads) out[want + i] = n + i;
+  for (int i = want + recent + threadIdx.x; i < p.kept_stride; i += choose::kThreads) out[i] = -1;
+  if (threadIdx.x == 0) p.kept_lens[b] = want + recent;
+  const float* totals = p.totals + (size_t)b * p.totals_stride + first;
+  choose::choose<uint32_t>(n, want, scratch, [&](int i) { return choose::key_of(totals[i]); },
+                           [&](int rank, int i) { out[rank] = i; });
+}
+
+// ---- move ------------------------------------------------------------------
+// A workgroup moves the rows of one (sequence, KV head, pool), kMovePasses x 256 pieces
+// of 16 bytes at a time: all of them loaded, a barrier, all of them stored.  In place
+// that is enough.  A row moves to a slot at or before its own, and what a later
+// round reads lies behind every slot that this one writes (kept ascends, so row j's
+// source is at least slot j), so only the rows of one round can stand in each
+// other's way.  To other blocks the rounds are workgroups of their own (chunks).
+// The rows are read and written once; nothing but their traffic bounds the move.
+constexpr int kPasses = kMovePasses;
+
+// The loads before this line have arrived in every thread of the workgroup.
+__device__ __forceinline__ void all_loaded() {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+}
+
+template <int D>
+__device__ __forceinline__ void move_rows(const CompactParams& p, int wg) {
+  constexpr int kRowThreads = D / 8;
+  constexpr int kRows = kMoveThreads / kRowThreads;                     // per pass
+  const int chunk = wg % p.chunks;
+  wg /= p.chunks;
+  const int g = wg % p.num_kv_heads;
+  wg /= p.num_kv_heads;
+  uint16_t* pool = wg & 1 ? p.v_pool : p.k_pool;
+  const int b = wg >> 1;
+  const int first = p.first_tokens ? clamped(p.first_tokens[b], p.max_ctx) : 0;
+  const int m = clamped(p.kept_lens[b], min(p.kept_stride, p.max_ctx - first));
+  const int32_t* kept = p.kept + (size_t)b * p.kept_stride;
+  const int32_t* from = p.block_tables + (size_t)b * p.bt_stride;
+  const int32_t* to = p.dst_tables ? p.dst_tables + (size_t)b * p.dst_stride : from;
+  const int to_blocks = p.dst_tables ? p.dst_stride : p.bt_stride;
+  const int row = threadIdx.x / kRowThreads, piece = threadIdx.x % kRowThreads;
+  auto slot = [&](int id, int t) {
+    return pool + (((size_t)clamped(id, p.num_blocks - 1) * p.num_kv_heads + g) * 16 + (t & 15)) * D + piece * 8;
+  };
+  for (int j0 = chunk * kPasses * kRows; j0 < m; j0 += p.chunks * kPasses * kRows) {   // uniform
+    uint4 x[kPasses];
+    uint16_t* dst[kPasses];
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i) {
+      const int j = j0 + i * kRows + row;
+      dst[i] = nullptr;
+      if (j < m && (first + j) >> 4 < to_blocks) {
+        const int s = clamped(kept[j], p.max_ctx - 1 - first) + first;
+        const uint16_t* src = slot(from[s >> 4], s);
+        dst[i] = slot(to[(first + j) >> 4], first + j);
+        if (dst[i] == src)
+          dst[i] = nullptr;                                             // it stays where it is
+        else
+          x[i] = *reinterpret_cast<const uint4*>(src);
+      }
+    }
+    all_loaded();
+#pragma unroll
+    for (int i = 0; i < kPasses; ++i)
+      if (dst[i]) *reinterpret_cast<uint4*>(dst[i]) = x[i];
+  }
+}
+
+// A sequence's totals, in the same way, and its new length.
+__device__ __forceinline__ void move_totals(const CompactParams& p, int b) {
+  const int first = p.first_tokens ? clamped(p.first_tokens[b], p.max_ctx) : 0;
+  const int m = clamped(p.kept_lens[b], min(p.kept_stride, p.max_ctx - first));
+  const int ctx = clamped(p.context_lens[b], p.max_ctx);
+  if (p.totals_out) {
+    const int32_t* kept = p.kept + (size_t)b * p.kept_stride;
+    const float* in = p.totals + (size_t)b * p.totals_stride;
+    float* out = p.totals_out + (size_t)b * p.totals_stride;
+    if (in != out)
+      for (int t = threadIdx.x; t < min(first, ctx); t += kMoveThreads) out[t] = in[t];
+    for (int j0 = 0; j0 < m; j0 += kPasses * kMoveThreads) {
+      float x[kPasses];
+#pragma unroll
+      for (int i = 0; i < kPasses; ++i) {
+        const int j = j0 + i * kMoveThreads + threadIdx.x;
+        x[i] = j < m ? in[first + clamped(kept[j], p.max_ctx - 1 - first)] : 0.f;
+      }
+      all_loaded();
+#pragma unroll
+      for (int i = 0; i < kPasses; ++i) {
+        const int j = j0 + i * kMoveThreads + threadIdx.x;
+        if (j < m) out[first + j] = x[i];
+      }
+    }
+    for (int t = first + m + threadIdx.x; t < ctx; t += kMoveThreads) out[t] = 0.f;
+  }
+  all_loaded();                                                         // new_lens may be context_lens
+  if (threadIdx.x == 0 && p.new_lens) p.new_lens[b] = first + m;
+}
+
+template <int D>
+__global__ void __launch_bounds__(kMoveThreads) compact_kernel(const CompactParams p) {
+  if ((int)blockIdx.x < p.batch)
+    move_totals(p, blockIdx.x);
+  else
+    move_rows<D>(p, blockIdx.x - p.batch);
+}
+
+}  // namespace
+
+hipError_t launch_keep(const KeepParams& p, hipStream_t stream) {
+  hipLaunchKernelGGL(keep_kernel, dim3((unsigned)p.batch), dim3(choose::kThreads), 0, stream, p);
+  return hipGetLastError();
+}
+
+hipError_t launch_compact(const CompactParams& p, hipStream_t stream) {
+  const dim3 grid((unsigned)(p.batch + (int64_t)p.batch * 2 * p.num_kv_heads * p.chunks));
+  if (p.head_dim == 128)
+    hipLaunchKernelGGL(compact_kernel<128>, grid, dim3(kMoveThreads), 0, stream, p);
+  else
+    hipLaunchKernelGGL(compact_kernel<64>, grid, dim3(kMoveThreads), 0, stream, p);
+  return hipGetLastError();
+}
+
+}  // namespace pa

@@ -7,6 +7,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+struct pa_kv_pool;
+
 namespace pa {
 
 constexpr int kRopeMaxDim = 256;        // largest head_dim of the row operators
@@ -87,10 +89,12 @@ struct BiasedParams {
   float c0, c1, c2, c3;
   float raw_max;
   float two_z;                   // 2 log2(e) |scale| / softcap
+  const int32_t* parents;        // [total_q], trees only
 };
 constexpr int kBiasedTileRows = 32;     // query rows (token x head) of a row tile
 constexpr int kBiasedWgRows = 128;      // rows of a workgroup in the form for long chunks
 constexpr int kCus = 256;               // compute units of the GPU
+constexpr int kTreeMostNodes = 256;     // of one sequence's tree
 
 // Blocks of one partition of a row tile that sees nblk blocks.  The plan's
 // part_blocks reach a window and the positions of a tile's rows; a prefix that sees
@@ -109,5 +113,17 @@ struct BiasedPlan {
   int32_t tiles, tile_rows, parts, part_blocks, big;
 };
 hipError_t launch_biased(const BiasedParams& p, hipStream_t stream);
+
+// A tree of drafted tokens (paged_attn_tokens.h) is planned, checked and
+// dispatched as a biased extend with its parents and its own kernels.
+using BiasedLaunch = hipError_t (*)(const BiasedParams&, hipStream_t);
+hipError_t launch_tree(const BiasedParams& p, hipStream_t stream);
+int biased_size(const pa_kv_pool* pool, int32_t batch, int32_t num_q_heads, int32_t max_context_len,
+                int32_t max_chunk, int32_t window, size_t* bytes_out, const char* fn);
+int biased_call(const pa_kv_pool* pool, const void* q, const int32_t* q_start, int32_t total_q, const int32_t* parents,
+                const int32_t* block_tables, int32_t bt_stride, const int32_t* context_lens, int32_t batch,
+                int32_t num_q_heads, float scale, float softcap, const float* slopes, int32_t window,
+                const int32_t* first_tokens, const int32_t* prefix_lens, int32_t max_context_len, int32_t max_chunk,
+                void* workspace, size_t workspace_bytes, void* out, void* stream, BiasedLaunch launch, const char* fn);
 
 }  // namespace pa

@@ -16,6 +16,7 @@
 
 #include "paged_attn.h"
 #include "paged_attn_ops.h"
+#include "paged_attn_tokens.h"
 
 #include <cstdint>
 #include <tuple>
@@ -127,9 +128,18 @@ const Entry kEntries[] = {
     PA_ENTRY(14, paged_attn_rope_append),
     PA_ENTRY(15, paged_attn_decode_biased),
     PA_ENTRY(16, paged_attn_extend_biased),
+    // paged_attn_tokens.h
+    PA_ENTRY(17, paged_attn_extend_tree),
+    PA_ENTRY(18, paged_attn_block_bounds),
+    PA_ENTRY(19, paged_attn_select_blocks),
+    PA_ENTRY(20, paged_attn_decode_selected),
+    PA_ENTRY(21, paged_attn_decode_weights),
+    PA_ENTRY(22, paged_attn_keep_heaviest),
+    PA_ENTRY(23, paged_attn_compact),
 };
 constexpr int kNumEntries = sizeof kEntries / sizeof kEntries[0];
-constexpr int kNumDecode = 13;   // those of paged_attn.h, NAMES; the others are OPS_NAMES
+constexpr int kNumDecode = 13;   // those of paged_attn.h, NAMES; up to kNumOps OPS_NAMES; the others are TOKENS_NAMES
+constexpr int kNumOps = 17;
 
 // bind({name: (address, ctypes call)}): every function above must be given.
 PyObject* bind(PyObject*, PyObject* calls) {
@@ -171,7 +181,8 @@ PyMODINIT_FUNC PyInit__pycall(void) {
     Py_XDECREF(names);
     return false;
   };
-  if (!add_names("NAMES", 0, kNumDecode) || !add_names("OPS_NAMES", kNumDecode, kNumEntries)) {
+  if (!add_names("NAMES", 0, kNumDecode) || !add_names("OPS_NAMES", kNumDecode, kNumOps) ||
+      !add_names("TOKENS_NAMES", kNumOps, kNumEntries)) {
     Py_DECREF(m);
     return nullptr;
   }
