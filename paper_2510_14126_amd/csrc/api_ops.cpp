@@ -315,6 +315,37 @@ pa::BiasedPlan biased_plan(int batch, int num_kv_heads, int group, int head_dim,
   return pl;
 }
 
+// The same for a tree of drafted tokens, by the bounds alone.  Its rows are few and its
+// tokens many, so the form of 128 rows, too, splits its tokens over workgroups, as many
+// as fill the two places of every CU.  It is taken for more than 64 rows of a (sequence,
+// KV head), half a tile, once tiles of 32 rows would walk a million tokens in all:
+// before that their chains, four times shorter, count more than reading a tile's tokens
+// four times.  32-row / 128-row form, 32 heads over 8, D = 128, in brackets rows and
+// walked tokens: one sequence of 30011 tokens and 16 nodes (64, 0.5M) 33 / 44 us, 24
+// (96, 0.7M) 43 / 49, 32 (128, 1.0M) 50 / 51, 64 heads and 61 nodes (488, 3.9M) 168 / 131
+// (256 workgroups instead of 512: 160); two of 500 and 24 (96, 0.03M) 12.5 / 17; one of
+// 1000 and 256 (1024, 0.3M) 20 / 29; 64 of about 2300 and 16 (64, 2.4M) 91 / 122, 24 (96,
+// 3.5M) 136 / 125; D = 64, heads over 4, 16 of 4000 and 16 (128, 1.0M) 35 / 33.
+constexpr int64_t kTreeBigRows = 65, kTreeBigTokens = 1 << 20, kTreeFill = 512;
+
+pa::BiasedPlan tree_plan(int batch, int num_kv_heads, int group, int head_dim, int max_ctx, int max_nodes) {
+  const int64_t rows = (int64_t)std::max(max_nodes, 1) * group;
+  const int64_t small_tiles = (rows + pa::kBiasedTileRows - 1) / pa::kBiasedTileRows;
+  pa::BiasedPlan pl;
+  pl.big = rows >= kTreeBigRows && batch * small_tiles * num_kv_heads >= kTreeBigTokens / std::max(max_ctx, 1);
+  const int64_t tile = pl.big ? pa::kBiasedWgRows : pa::kBiasedTileRows;
+  pl.tiles = (int32_t)((rows + tile - 1) / tile);
+  pl.tile_rows = (int32_t)std::min(rows, tile);
+  const int64_t wgs = std::max<int64_t>(1, (int64_t)batch * pl.tiles * num_kv_heads);
+  const int64_t blocks = std::max<int64_t>(1, ((int64_t)max_ctx + PA_BLOCK_SIZE - 1) / PA_BLOCK_SIZE);
+  const int64_t fill = pl.big ? kTreeFill : head_dim == 64 ? kFillWorkgroups64 : kFillWorkgroups128;
+  const int64_t parts = std::max<int64_t>(1, fill / wgs);
+  const int64_t per = parts == 1 || blocks <= kWholeBlocks ? blocks : std::max(kLeastBlocks, (blocks + 2 * parts - 1) / (2 * parts) * 2);
+  pl.parts = (int32_t)((blocks + per - 1) / per);
+  pl.part_blocks = (int32_t)per;
+  return pl;
+}
+
 size_t biased_part_o_bytes(const pa::BiasedPlan& pl, int64_t slots, int32_t head_dim) {
   return pl.parts > 1 ? (size_t)slots * pl.parts * pl.tile_rows * head_dim * sizeof(float) : 0;
 }
@@ -324,7 +355,8 @@ size_t biased_lse_bytes(const pa::BiasedPlan& pl, int64_t slots) {
 
 // Geometry and plan of a biased call, and its number of row tiles.
 int plan_biased(const pa_kv_pool* pool, int32_t batch, int32_t num_q_heads, int32_t max_context_len,
-                int32_t max_chunk, int32_t window, int64_t total_q, pa::BiasedPlan* pl, int64_t* slots, const char* fn) {
+                int32_t max_chunk, int32_t window, int64_t total_q, bool tree, pa::BiasedPlan* pl, int64_t* slots,
+                const char* fn) {
   if (!pool) return fail(PA_EINVAL, "%s: pool is NULL", fn);
   if (batch < 0) return fail(PA_EINVAL, "%s: batch = %d < 0", fn, batch);
   if (num_q_heads <= 0 || num_q_heads % pool->num_kv_heads != 0)
@@ -343,8 +375,9 @@ int plan_biased(const pa_kv_pool* pool, int32_t batch, int32_t num_q_heads, int3
   *slots = (int64_t)batch * tiles;
   if (*slots > 0x7fffffffLL / pool->num_kv_heads) return fail(PA_EINVAL, "%s: grid too large", fn);
   *slots *= pool->num_kv_heads;
-  *pl = biased_plan(batch, pool->num_kv_heads, group, pool->head_dim, max_context_len, max_chunk, window,
-                    total_q);
+  *pl = tree ? tree_plan(batch, pool->num_kv_heads, group, pool->head_dim, max_context_len, max_chunk)
+             : biased_plan(batch, pool->num_kv_heads, group, pool->head_dim, max_context_len, max_chunk, window, total_q);
+  if (tree) *slots = (int64_t)batch * pl->tiles * pool->num_kv_heads;
   if (*slots * pl->parts > 0x7fffffffLL || (pl->parts > 1 && *slots * pl->tile_rows > 0x7fffffffLL))
     return fail(PA_EINVAL, "%s: grid too large", fn);
   return PA_OK;
@@ -357,11 +390,11 @@ int plan_biased(const pa_kv_pool* pool, int32_t batch, int32_t num_q_heads, int3
 namespace pa {
 
 int biased_size(const pa_kv_pool* pool, int32_t batch, int32_t num_q_heads, int32_t max_context_len,
-                int32_t max_chunk, int32_t window, size_t* bytes_out, const char* fn) {
+                int32_t max_chunk, int32_t window, bool tree, size_t* bytes_out, const char* fn) {
   if (!bytes_out) return fail(PA_EINVAL, "%s: NULL output pointer", fn);
   BiasedPlan pl;
   int64_t slots = 0;
-  const int rc = plan_biased(pool, batch, num_q_heads, max_context_len, max_chunk, window, 0, &pl, &slots, fn);
+  const int rc = plan_biased(pool, batch, num_q_heads, max_context_len, max_chunk, window, 0, tree, &pl, &slots, fn);
   if (rc) return rc;
   *bytes_out = biased_part_o_bytes(pl, slots, pool->head_dim) + biased_lse_bytes(pl, slots);
   return PA_OK;
@@ -374,7 +407,7 @@ int biased_call(const pa_kv_pool* pool, const void* q, const int32_t* q_start, i
                 void* workspace, size_t workspace_bytes, void* out, void* stream, BiasedLaunch launch, const char* fn) {
   pa::BiasedPlan pl;
   int64_t slots = 0;
-  int rc = plan_biased(pool, batch, num_q_heads, max_context_len, max_chunk, window, total_q, &pl, &slots, fn);
+  int rc = plan_biased(pool, batch, num_q_heads, max_context_len, max_chunk, window, total_q, parents != nullptr, &pl, &slots, fn);
   if (rc) return rc;
   if (total_q < 0) return fail(PA_EINVAL, "%s: total_q = %d < 0", fn, total_q);
   const int64_t need_bt = ((int64_t)max_context_len + PA_BLOCK_SIZE - 1) / PA_BLOCK_SIZE;
@@ -468,7 +501,7 @@ extern "C" {
 
 int paged_attn_biased_workspace_size(const pa_kv_pool* pool, int32_t batch, int32_t num_q_heads,
                                      int32_t max_context_len, int32_t max_chunk, int32_t window, size_t* bytes_out) {
-  return pa::biased_size(pool, batch, num_q_heads, max_context_len, max_chunk, window, bytes_out,
+  return pa::biased_size(pool, batch, num_q_heads, max_context_len, max_chunk, window, false, bytes_out,
                          "paged_attn_biased_workspace_size");
 }
 

@@ -189,7 +189,7 @@ int paged_attn_tree_workspace_size(const pa_kv_pool* pool, int32_t batch, int32_
   const char* fn = "paged_attn_tree_workspace_size";
   if (max_nodes > PA_TREE_MAX_NODES)
     return fail(PA_EUNSUPPORTED, "%s: max_nodes = %d > %d", fn, max_nodes, PA_TREE_MAX_NODES);
-  return pa::biased_size(pool, batch, num_q_heads, max_context_len, max_nodes, 0, bytes_out, fn);
+  return pa::biased_size(pool, batch, num_q_heads, max_context_len, max_nodes, 0, true, bytes_out, fn);
 }
 
 int paged_attn_extend_tree(const pa_kv_pool* pool, const void* q, const int32_t* q_start, int32_t total_q,
@@ -266,7 +266,7 @@ int paged_attn_select_blocks(const pa_kv_pool* pool, const void* q, const void* 
   if (!aligned(block_tables, 4) || !aligned(context_lens, 4) || !aligned(selected, 4))
     return fail(PA_EINVAL, "%s: block_tables/context_lens/selected are not 4-byte aligned", fn);
   const int64_t rows = (int64_t)batch * pool->num_kv_heads, blocks = blocks_of(max_context_len);
-  if ((rc = check_grid(rows, 1024, fn)) || (rc = check_grid(rows * ((blocks + 127) / 128), 256, fn)) ||
+  if ((rc = check_grid(rows, 1024, fn)) || (rc = check_grid(rows * ((blocks + 63) / 64), 256, fn)) ||
       (rc = check_workspace(workspace, workspace_bytes, need, fn)))
     return rc;
   pa::BlocksParams p{};

@@ -830,7 +830,8 @@ __device__ __forceinline__ bool ranked_tile(const BiasedParams& p, int i, int& b
   return true;
 }
 
-// TREE: kTreeBytes<kBiasedWgRows> of LDS follow kBigLdsBytes.
+// TREE: kTreeBytes<kBiasedWgRows> of LDS follow kBigLdsBytes, and the tokens may be
+// split over workgroups (parts).
 template <int D, bool CAP, bool BIAS, bool TREE = false>
 __device__ __forceinline__ void big_body(const BiasedParams& p, int wg, lds_u8_t* smem) {
   using Cols = Columns<D, CAP, BIAS, TREE>;
@@ -844,15 +845,26 @@ __device__ __forceinline__ void big_body(const BiasedParams& p, int wg, lds_u8_t
   // A chunk's last rows see the most tokens: they start first.
   int tile = p.tiles - 1 - wg % p.tiles;
   int b = wg / p.tiles;
+  int part = 0;
+  if constexpr (TREE) {
+    part = b / p.batch;
+    b = b % p.batch;
+  }
   Chunk c;
-  if (p.ranked) {
+  if (!TREE && p.ranked) {
     if (!ranked_tile(p, wg, b, c, tile)) return;       // whole workgroup
   } else {
     c = chunk_of(p, b);
   }
   const int rows = c.len * p.group;
   if (tile * kBiasedWgRows >= rows) return;            // whole workgroup: no rows here
-  const int row0 = tile * kBiasedWgRows + kBiasedTileRows * wave;
+  // Which 32 of the rows the wavefront takes.  A tree's tile is seldom full: a
+  // wavefront without rows computes nothing, and since wavefront i of either of a CU's
+  // two workgroups runs on its SIMD i, every other workgroup turns the rows by two, so
+  // that its idle wavefronts meet the other's busy ones.
+  const int turn = TREE ? (wave + 2 * (int)(blockIdx.x / kCus & 1)) & 3 : wave;
+  const int row0 = tile * kBiasedWgRows + kBiasedTileRows * turn;
+  const bool busy = !TREE || row0 < rows;
 
   // A column without a row repeats the workgroup's first and is not written.
   const int R = row0 + n < rows ? row0 + n : tile * kBiasedWgRows;
@@ -886,15 +898,28 @@ __device__ __forceinline__ void big_body(const BiasedParams& p, int wg, lds_u8_t
     __syncthreads();                                   // `range` is used again
   }
   const int from_pos = c.first + tile * kBiasedWgRows / p.group;   // position of the workgroup's first row
-  const int j0 = lo >> 4;
-  const int cnt = hi > lo ? ((hi + 15) >> 4) - j0 : 0;
+  int j0 = lo >> 4;
+  int cnt = hi > lo ? ((hi + 15) >> 4) - j0 : 0;
+  bool split = false;                                  // else the first partition writes the output
+  size_t slot = 0;                                     // of its first row's partial results
+  if constexpr (TREE) {
+    slot = ((((size_t)b * p.tiles + tile) * p.num_kv_heads + g) * p.parts + part) * p.tile_rows + turn * kBiasedTileRows;
+    const int per = p.parts > 1 ? p.part_blocks : cnt;
+    split = cnt > per;
+    j0 += part * per;
+    cnt = min(per, cnt - part * per);
+    if (cnt <= 0 && part > 0) {
+      if (lane < kBiasedTileRows && turn * kBiasedTileRows + lane < p.tile_rows) p.part_lse[slot + lane] = -__builtin_inff();
+      return;                                          // whole workgroup
+    }
+  }
 
   Cols C;
   C.init(p, row);
   if constexpr (TREE) {
     lds_u32_t* words = reinterpret_cast<lds_u32_t*>(smem + kBigLdsBytes<D>);
     tree_rows<kBiasedWgRows>(p, c, tile * kBiasedWgRows, words, reinterpret_cast<lds_u16_t*>(smem));
-    C.tree = words + wave * kBiasedTileRows * kTreePitch;
+    C.tree = words + turn * kBiasedTileRows * kTreePitch;
     C.drafted = c.first;
   }
   auto query = [&](int s) { return q[s]; };
@@ -973,10 +998,13 @@ __device__ __forceinline__ void big_body(const BiasedParams& p, int wg, lds_u8_t
   load(2);
   __syncthreads();
   auto linear = [&](int s) { return first_of(s) + kTokens <= from_pos + 1; };
-  floatx16_t raw = C.scores(smem, h, n, query);
-  floatx16_t a = C.shape(p, raw, first_of(0), h);
-  C.reshape(p, a, raw, first_of(0), edge(0), linear(0), h);
-  C.raise(a, rowv, h, n);
+  floatx16_t raw, a;
+  if (busy) {
+    raw = C.scores(smem, h, n, query);
+    a = C.shape(p, raw, first_of(0), h);
+    C.reshape(p, a, raw, first_of(0), edge(0), linear(0), h);
+    C.raise(a, rowv, h, n);
+  }
   for (int s0 = 0; s0 < nstage; s0 += kSlots) {
 #pragma unroll
     for (int u = 0; u < kSlots; ++u) {
@@ -984,12 +1012,14 @@ __device__ __forceinline__ void big_body(const BiasedParams& p, int wg, lds_u8_t
       if (s < nstage) {                                // uniform over the workgroup
         publish(s + 2, (u + 2) % kSlots);
         load(s + 3);
-        raw = C.scores(smem + (u + 1) % kSlots * kStageBytes<D>, h, n, query);
-        C.attend(a, smem + u * kStageBytes<D>, lane);
-        a = C.shape(p, raw, first_of(s + 1), h);
-        if (s + 1 < nstage) {
-          C.reshape(p, a, raw, first_of(s + 1), edge(s + 1), linear(s + 1), h);
-          C.raise(a, rowv, h, n);
+        if (busy) {
+          raw = C.scores(smem + (u + 1) % kSlots * kStageBytes<D>, h, n, query);
+          C.attend(a, smem + u * kStageBytes<D>, lane);
+          a = C.shape(p, raw, first_of(s + 1), h);
+          if (s + 1 < nstage) {
+            C.reshape(p, a, raw, first_of(s + 1), edge(s + 1), linear(s + 1), h);
+            C.raise(a, rowv, h, n);
+          }
         }
         __syncthreads();
       }
@@ -1012,6 +1042,20 @@ __device__ __forceinline__ void big_body(const BiasedParams& p, int wg, lds_u8_t
   const float lcol = lx + ly;
   float inv[16];
   Cols::per_row(rowv, h, n, lcol == 0.f ? 0.f : 1.0f / lcol, inv);
+  if constexpr (TREE) {
+    if (p.parts > 1 && h == 0 && turn * kBiasedTileRows + n < p.tile_rows)
+      p.part_lse[slot + n] = !split ? kWhole : (lcol == 0.f ? -__builtin_inff() : C.m + log2f(lcol));
+    if (split) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int at = 8 * (r >> 2) + 4 * h + (r & 3);
+        if (row0 + at < rows)
+#pragma unroll
+          for (int j = 0; j < D / 32; ++j) store_partial(p.part_o + (slot + at) * D + 32 * j + n, C.o[j][r] * inv[r]);
+      }
+      return;
+    }
+  }
   lds_u8_t* out = smem + wave * (kBiasedTileRows * D * 2);
 #pragma unroll
   for (int r = 0; r < 16; ++r)
@@ -1040,7 +1084,7 @@ __device__ __forceinline__ void big_body(const BiasedParams& p, int wg, lds_u8_t
 // dealt to the wavefronts in groups of kGroup that are loaded together, and the
 // wavefronts' sums are added in order through LDS.
 constexpr int kGroup = 8;
-template <int D, int NW>
+template <int D, int NW, int ROWS = kBiasedTileRows>
 __device__ __forceinline__ void merge_body(const BiasedParams& p, int slot0, int r, int wave, lds_f32_t* smem) {
   constexpr int DPL = D / 64;
   const int lane = threadIdx.x & 63;
@@ -1065,7 +1109,7 @@ __device__ __forceinline__ void merge_body(const BiasedParams& p, int slot0, int
   };
   if constexpr (NW > 1) load_group(wave * kGroup, p.parts > wave * kGroup ? ~0ull >> (64 - min(p.parts - wave * kGroup, 64)) : 0);
   const Chunk c = chunk_of(p, b);
-  const int R = tile * kBiasedTileRows + r;
+  const int R = tile * ROWS + r;
   if (R >= c.len * p.group) return;                             // all wavefronts of the row
   if (__int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x0))) == kWhole) return;
   float mx = x0;

@@ -3,6 +3,8 @@
 #include "choose_body.h"
 #include "tokens.h"
 
+#include <algorithm>
+
 namespace pa {
 namespace {
 
@@ -79,15 +81,42 @@ __global__ void __launch_bounds__(256) bounds_kernel(const BlocksParams p, int b
 // that of its scalar fp32, and what bounds the pass is reading the bounds, 4 D bytes
 // a block and KV head, a sixteenth of its keys and values.
 //
-// D / 4 lanes read a block's bounds, 16 bytes each, kLoads loads in flight per
-// wavefront; their partial sums are exchanged so that each step halves the blocks a
-// lane still holds: 16 additions for 16 blocks.
-constexpr int kLoads = 16;
+// D / 4 lanes read a block's bounds, 16 bytes each; a wavefront has kLoads loads in
+// flight for its next round while it sums the blocks of this one.  The lanes' partial
+// sums are exchanged so that each step halves the blocks a lane still holds.
+constexpr int kLoads = 8;
 template <int D> constexpr int kGroups = 64 / (D / 4);                // blocks per load
-template <int D> constexpr int kWaveBlocks = kLoads * kGroups<D>;     // blocks per wavefront and round
+template <int D> constexpr int kRoundBlocks = kLoads * kGroups<D>;    // blocks per wavefront and round
+constexpr int kWaves = 4;
+// Rounds of a wavefront: as many as leave kFillWaves wavefronts (four times what the
+// GPU holds), so that the chain of loads before a wavefront's first round (length,
+// table, bounds) and its sums of q are paid once for several.
+constexpr int kFillWaves = 16 * 1024, kMostRounds = 16;
 
-__device__ __forceinline__ double exchanged(double x, int m) {
-  return __builtin_bit_cast(double, __shfl_xor(__builtin_bit_cast(unsigned long long, x), m));
+template <int CTRL>
+__device__ __forceinline__ double moved(double x) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_mov_dpp((int)(uint32_t)u, CTRL, 0xf, 0xf, true);
+  const uint32_t hi = (uint32_t)__builtin_amdgcn_mov_dpp((int)(uint32_t)(u >> 32), CTRL, 0xf, 0xf, true);
+  return __builtin_bit_cast(double, ((uint64_t)hi << 32) | lo);
+}
+constexpr int kDppHalfMirror = 0x141;   // lane i of eight gets lane 7 - i's
+
+// a of the lanes with the bit M clear and b of those with it set, each plus the same
+// value of a lane that has the bit the other way round.  (Which one does not matter:
+// the lanes below M are summed later.)
+template <int M>
+__device__ __forceinline__ double folded(double a, double b, int lane) {
+  if constexpr (M == 16) {
+    const uint64_t x = __builtin_bit_cast(uint64_t, a), y = __builtin_bit_cast(uint64_t, b);
+    const auto lo = __builtin_amdgcn_permlane16_swap((uint32_t)x, (uint32_t)y, false, false);
+    const auto hi = __builtin_amdgcn_permlane16_swap((uint32_t)(x >> 32), (uint32_t)(y >> 32), false, false);
+    return __builtin_bit_cast(double, ((uint64_t)hi[0] << 32) | lo[0]) + __builtin_bit_cast(double, ((uint64_t)hi[1] << 32) | lo[1]);
+  } else {
+    constexpr int kCtrl = M == 8 ? kDppRowRor8 : (M == 4 ? kDppHalfMirror : (M == 2 ? kDppQuadXor2 : kDppQuadXor1));
+    const bool up = (lane & M) != 0;
+    return (up ? b : a) + moved<kCtrl>(up ? a : b);
+  }
 }
 
 // Candidates of a sequence: how many blocks lie between its first and last ones;
@@ -97,33 +126,49 @@ __device__ __forceinline__ int candidates(const BlocksParams& p, int nblk) {
 }
 
 template <int D>
-__global__ void __launch_bounds__(256) score_kernel(const BlocksParams p) {
+__global__ void __launch_bounds__(64 * kWaves) score_kernel(const BlocksParams p, int rounds) {
   constexpr int kLanes = D / 4;                    // lanes per block
+  constexpr int kPer = kRoundBlocks<D>;
   const int lane = threadIdx.x & 63;
   const int wave = wave_uniform(threadIdx.x >> 6);
   int wg = blockIdx.x;
   const int g = wg % p.num_kv_heads;
   wg /= p.num_kv_heads;
   const int b = wg % p.batch;
-  const int base = (wg / p.batch * 4 + wave) * kWaveBlocks<D>;
-  const int ctx = clamped(p.context_lens[b], p.max_ctx);
-  const int n = candidates(p, (ctx + 15) >> 4);
-  if (base >= n) return;
-  const int32_t* table = p.block_tables + (size_t)b * p.bt_stride + p.first_blocks + base;
-  const int ids = lane < kWaveBlocks<D> && base + lane < n ? clamped(table[lane], p.num_blocks - 1) : 0;
+  const int base = (wg / p.batch * kWaves + wave) * rounds * kPer;
   const int part = lane / kLanes, piece = lane % kLanes;
-  uint4 x[kLoads];
-#pragma unroll
-  for (int i = 0; i < kLoads; ++i) {
-    const size_t id = (size_t)__shfl(ids, i * kGroups<D> + part);
-    x[i] = *reinterpret_cast<const uint4*>(p.bounds + (id * p.num_kv_heads + g) * (2 * D) + piece * 8);
-  }
   // the lane's side: pieces of the least values meet the negative parts of q
   const bool upper = piece >= kLanes / 2;
-  double q[8] = {0, 0, 0, 0, 0, 0, 0, 0};
   const uint16_t* q_row = p.q + ((size_t)b * p.num_kv_heads + g) * p.group * D + piece % (kLanes / 2) * 8;
+  uint4 first_row = *reinterpret_cast<const uint4*>(q_row);
+  const int ctx = clamped(p.context_lens[b], p.max_ctx);
+  const int n = candidates(p, (ctx + 15) >> 4);
+  const int end = min(n, base + rounds * kPer);
+  if (base >= end) return;
+  const int32_t* table = p.block_tables + (size_t)b * p.bt_stride + p.first_blocks;
+  const uint16_t* bounds = p.bounds + (size_t)g * (2 * D) + piece * 8;
+  const size_t stride = (size_t)p.num_kv_heads * (2 * D);
+
+  // 64 table entries at a time, and the 64 behind them
+  auto ids_from = [&](int at) { return at + lane < end ? clamped(table[at + lane], p.num_blocks - 1) : 0; };
+  int ids = ids_from(base), ids_next = ids_from(base + 64);
+  auto load = [&](uint4 (&x)[kLoads], int at) {    // at - base: a multiple of kPer, which divides 64
+    if (at > base && ((at - base) & 63) == 0) {
+      ids = ids_next;
+      ids_next = ids_from(at + 64);
+    }
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const size_t id = (size_t)__shfl(ids, ((at - base) & 63) + i * kGroups<D> + part);
+      x[i] = *reinterpret_cast<const uint4*>(bounds + id * stride);
+    }
+  };
+  uint4 x[2][kLoads];
+  load(x[0], base);
+
+  double q[8] = {0, 0, 0, 0, 0, 0, 0, 0};
   for (int h = 0; h < p.group; ++h) {
-    const uint4 y = *reinterpret_cast<const uint4*>(q_row + (size_t)h * D);
+    const uint4 y = h == 0 ? first_row : *reinterpret_cast<const uint4*>(q_row + (size_t)h * D);
     const uint32_t w[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
     for (int d = 0; d < 8; ++d) {
@@ -131,36 +176,55 @@ __global__ void __launch_bounds__(256) score_kernel(const BlocksParams p) {
       q[d] += (double)((upper ? z < 0.f : z > 0.f) ? 0.f : z);        // NaN stays
     }
   }
-  double v[kLoads];
+
+  uint64_t* keys = p.keys + ((size_t)b * p.num_kv_heads + g) * p.key_blocks;
+  auto score = [&](const uint4 (&y)[kLoads], int at) {
+    double v[kLoads];
 #pragma unroll
-  for (int i = 0; i < kLoads; ++i) {
-    const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-    v[i] = 0.0;
+    for (int i = 0; i < kLoads; ++i) {
+      const uint32_t w[4] = {y[i].x, y[i].y, y[i].z, y[i].w};
+      v[i] = 0.0;
 #pragma unroll
-    for (int d = 0; d < 8; ++d) v[i] = fma(q[d], (double)(d & 1 ? bf16_hi(w[d / 2]) : bf16_lo(w[d / 2])), v[i]);
-  }
-  int load = 0, m = kLanes / 2;
-#pragma unroll
-  for (int half = kLoads / 2; half >= 1; half /= 2) {
-    const bool up = (lane & m) != 0;
-#pragma unroll
-    for (int i = 0; i < half; ++i) {
-      const double keep = up ? v[i + half] : v[i], give = up ? v[i] : v[i + half];
-      v[i] = keep + exchanged(give, m);
+      for (int d = 0; d < 8; ++d) v[i] = fma(q[d], (double)(d & 1 ? bf16_hi(w[d / 2]) : bf16_lo(w[d / 2])), v[i]);
     }
-    load += up ? half : 0;
-    m >>= 1;
+    // lane bits from the block's highest on choose which half stays
+    int i;
+    if constexpr (kLanes == 32) {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = folded<16>(v[k], v[k + 4], lane);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) v[k] = folded<8>(v[k], v[k + 2], lane);
+      v[0] = folded<4>(v[0], v[1], lane);
+      v[0] += moved<kDppQuadXor2>(v[0]);
+      i = ((lane & 16) >> 2) | ((lane & 8) >> 2) | ((lane & 4) >> 2);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = folded<8>(v[k], v[k + 4], lane);
+#pragma unroll
+      for (int k = 0; k < 2; ++k) v[k] = folded<4>(v[k], v[k + 2], lane);
+      v[0] = folded<2>(v[0], v[1], lane);
+      i = ((lane & 8) >> 1) | ((lane & 4) >> 1) | ((lane & 2) >> 1);
+    }
+    v[0] += moved<kDppQuadXor1>(v[0]);
+    const int block = at + i * kGroups<D> + part;
+    if (block < end && lane % (kLanes / kLoads) == 0) keys[block] = choose::key_of(v[0]);
+  };
+  for (int at = base; at < end; at += 2 * kPer) {
+    if (at + kPer < end) load(x[1], at + kPer);    // uniform
+    score(x[0], at);
+    if (at + kPer >= end) break;
+    if (at + 2 * kPer < end) load(x[0], at + 2 * kPer);
+    score(x[1], at + kPer);
   }
-  if constexpr (kLanes == 32) v[0] += exchanged(v[0], 1);
-  const int block = load * kGroups<D> + part;
-  if (base + block < n && (kLanes < 32 || (lane & 1) == 0))
-    p.keys[((size_t)b * p.num_kv_heads + g) * p.key_blocks + base + block] = choose::key_of(v[0]);
 }
 
 // ---- choice ----------------------------------------------------------------
-// One workgroup per (sequence, KV head); the keys come from L2 once per digit.
+// One workgroup per (sequence, KV head).
+constexpr int kFewKeys = 2048, kManyKeys = 16384;
+template <int CAPACITY>
 __global__ void __launch_bounds__(choose::kThreads) select_kernel(const BlocksParams p) {
   __shared__ choose::Scratch scratch;
+  __shared__ uint64_t room[CAPACITY];
   const int g = blockIdx.x % p.num_kv_heads, b = blockIdx.x / p.num_kv_heads;
   const size_t row = (size_t)b * p.num_kv_heads + g;
   const int ctx = clamped(p.context_lens[b], p.max_ctx);
@@ -176,8 +240,8 @@ __global__ void __launch_bounds__(choose::kThreads) select_kernel(const BlocksPa
   for (int i = threadIdx.x; i < p.last_blocks; i += choose::kThreads)
     out[p.max_blocks - p.last_blocks + i] = nblk - p.last_blocks + i;
   const uint64_t* keys = p.keys + row * p.key_blocks;
-  choose::choose<uint64_t>(n, want, scratch, [&](int i) { return keys[i]; },
-                           [&](int rank, int i) { out[p.first_blocks + rank] = p.first_blocks + i; });
+  choose::choose<uint64_t, CAPACITY>(n, want, scratch, room, [&](int i) { return keys[i]; },
+                                     [&](int rank, int i) { out[p.first_blocks + rank] = p.first_blocks + i; });
 }
 
 }  // namespace
@@ -196,15 +260,20 @@ hipError_t launch_bounds(const BlocksParams& p, hipStream_t stream) {
 hipError_t launch_select(const BlocksParams& p, hipStream_t stream) {
   const int64_t rows = (int64_t)p.batch * p.num_kv_heads;
   if (p.key_blocks > p.max_blocks) {                   // else every sequence attends to all of its blocks
-    const int per = 4 * (p.head_dim == 128 ? kWaveBlocks<128> : kWaveBlocks<64>);
-    const int64_t n = p.key_blocks - p.first_blocks - p.last_blocks;
-    const dim3 grid((unsigned)(rows * ((n + per - 1) / per)));
+    const int per = p.head_dim == 128 ? kRoundBlocks<128> : kRoundBlocks<64>;
+    const int64_t n = (p.key_blocks - p.first_blocks - p.last_blocks + per - 1) / per;      // rounds of a row
+    const int rounds = (int)std::min<int64_t>(kMostRounds, std::max<int64_t>(1, rows * n / kFillWaves));
+    const dim3 grid((unsigned)(rows * ((n + kWaves * rounds - 1) / (kWaves * rounds)))), wg(64 * kWaves);
     if (p.head_dim == 128)
-      hipLaunchKernelGGL(score_kernel<128>, grid, dim3(256), 0, stream, p);
+      hipLaunchKernelGGL(score_kernel<128>, grid, wg, 0, stream, p, rounds);
     else
-      hipLaunchKernelGGL(score_kernel<64>, grid, dim3(256), 0, stream, p);
+      hipLaunchKernelGGL(score_kernel<64>, grid, wg, 0, stream, p, rounds);
   }
-  hipLaunchKernelGGL(select_kernel, dim3((unsigned)rows), dim3(choose::kThreads), 0, stream, p);
+  const dim3 grid((unsigned)rows), wg(choose::kThreads);
+  if (p.key_blocks - p.first_blocks - p.last_blocks <= kFewKeys)
+    hipLaunchKernelGGL(select_kernel<kFewKeys>, grid, wg, 0, stream, p);
+  else
+    hipLaunchKernelGGL(select_kernel<kManyKeys>, grid, wg, 0, stream, p);
   return hipGetLastError();
 }
 

@@ -42,20 +42,22 @@ __device__ __forceinline__ uint32_t key_of(float x) {
 }
 
 // load(i): key i < n.  emit(rank, i): key i is one of the chosen, rank < want.  Every
-// thread of the workgroup calls it; 0 <= want <= n.
+// thread of the workgroup calls it, with the same n and 0 < want < n.
 template <typename Key, typename Load, typename Emit>
-__device__ __forceinline__ void choose(int n, int want, Scratch& s, const Load& load, const Emit& emit) {
+__device__ __forceinline__ void choose_some(int n, int want, Scratch& s, const Load& load, const Emit& emit) {
   const int lane = threadIdx.x & 63;
   const int wave = wave_uniform(threadIdx.x >> 6);
-  if (want <= 0) return;
-  if (want >= n) {
-    for (int i = threadIdx.x; i < n; i += kThreads) emit(i, i);
-    return;
-  }
   constexpr int kBits = 8 * sizeof(Key);
   const Key key0 = load(0);
+  // a wavefront's stretch of the keys, whole groups of 64
+  const int stretch = (n + kThreads - 1) / kThreads * 64;
+  const int from = min(n, wave * stretch), to = min(n, from + stretch);
+  // f(i, key, in) for the lane's keys, all lanes together; in: there is a key i
+  auto each = [&](const auto& f) {
+    for (int i0 = from; i0 < to; i0 += 64) f(i0 + lane, i0 + lane < to ? load(i0 + lane) : (Key)0, i0 + lane < to);
+  };
   uint64_t any = 0;
-  for (int i = threadIdx.x; i < n; i += kThreads) any |= (uint64_t)(load(i) ^ key0);
+  each([&](int, Key k, bool in) { any |= in ? (uint64_t)(k ^ key0) : 0; });
 #pragma unroll
   for (int m = 1; m < 64; m <<= 1) any |= __shfl_xor((unsigned long long)any, m);
   if (lane == 0) s.any[wave] = any;
@@ -74,10 +76,9 @@ __device__ __forceinline__ void choose(int n, int want, Scratch& s, const Load& 
     const int lo = hi - bits;
     if (threadIdx.x < 256) s.hist[threadIdx.x] = 0;
     __syncthreads();
-    for (int i = threadIdx.x; i < n; i += kThreads) {
-      const Key k = load(i);
-      if (top(k) == fixed) atomicAdd(&s.hist[(uint32_t)(k >> lo) & ((1u << bits) - 1)], 1u);
-    }
+    each([&](int, Key k, bool in) {
+      if (in && top(k) == fixed) atomicAdd(&s.hist[(uint32_t)(k >> lo) & ((1u << bits) - 1)], 1u);
+    });
     __syncthreads();
     if (wave == 0) {
       // lane: digits 255 - 4 lane down to 252 - 4 lane, and the count of those above
@@ -111,16 +112,11 @@ __device__ __forceinline__ void choose(int n, int want, Scratch& s, const Load& 
     hi = lo;
   }
 
-  // stretches of whole groups of 64 keys
-  const int stretch = (n + kThreads - 1) / kThreads * 64;
-  const int from = wave * stretch, to = min(n, from + stretch);
   int above = 0, equal = 0;
-  for (int i0 = from; i0 < to; i0 += 64) {
-    const bool in = i0 + lane < to;
-    const Key k = in ? top(load(i0 + lane)) : (Key)0;
-    above += __builtin_popcountll(__builtin_amdgcn_ballot_w64(in && k > fixed));
-    equal += __builtin_popcountll(__builtin_amdgcn_ballot_w64(in && k == fixed));
-  }
+  each([&](int, Key k, bool in) {
+    above += __builtin_popcountll(__builtin_amdgcn_ballot_w64(in && top(k) > fixed));
+    equal += __builtin_popcountll(__builtin_amdgcn_ballot_w64(in && top(k) == fixed));
+  });
   if (lane == 0) {
     s.above[wave] = above;
     s.equal[wave] = equal;
@@ -133,15 +129,37 @@ __device__ __forceinline__ void choose(int n, int want, Scratch& s, const Load& 
     equal += s.equal[w];
   }
   const uint64_t below = (1ull << lane) - 1;
-  for (int i0 = from; i0 < to; i0 += 64) {
-    const bool in = i0 + lane < to;
-    const Key k = in ? top(load(i0 + lane)) : (Key)0;
-    const uint64_t a = __builtin_amdgcn_ballot_w64(in && k > fixed), e = __builtin_amdgcn_ballot_w64(in && k == fixed);
+  each([&](int i, Key k, bool in) {
+    const Key t = top(k);
+    const uint64_t a = __builtin_amdgcn_ballot_w64(in && t > fixed), e = __builtin_amdgcn_ballot_w64(in && t == fixed);
     const int a_rank = above + __builtin_popcountll(a & below), e_rank = equal + __builtin_popcountll(e & below);
-    if (in && (k > fixed || (k == fixed && e_rank < need))) emit(a_rank + min(e_rank, need), i0 + lane);
+    if (in && (t > fixed || (t == fixed && e_rank < need))) emit(a_rank + min(e_rank, need), i);
     above += __builtin_popcountll(a);
     equal += __builtin_popcountll(e);
+  });
+}
+
+// The same for 0 <= want <= n.  Up to CAPACITY keys wait in LDS (`room`), which takes
+// the passes' loads from L2 out of the chain.
+// (In registers they are slower: the unrolled passes are code that is fetched from L2
+// as it runs, once, 11.7 / 9.3 us for 512 rows of 250..1800 keys.)
+template <typename Key, int CAPACITY, typename Load, typename Emit>
+__device__ __forceinline__ void choose(int n, int want, Scratch& s, Key* room, const Load& load, const Emit& emit) {
+  if (want <= 0) return;
+  if (want >= n) {
+    for (int i = threadIdx.x; i < n; i += kThreads) emit(i, i);
+    return;
   }
+  if (n > CAPACITY) {
+    choose_some<Key>(n, want, s, load, emit);
+    return;
+  }
+  const int stretch = (n + kThreads - 1) / kThreads * 64;
+  const int from = min(n, wave_uniform(threadIdx.x >> 6) * stretch), to = min(n, from + stretch);
+#pragma unroll 4
+  for (int i = from + (threadIdx.x & 63); i < to; i += 64) room[i] = load(i);
+  __syncthreads();
+  choose_some<Key>(n, want, s, [&](int i) { return room[i]; }, emit);
 }
 
 }  // namespace choose

@@ -9,10 +9,12 @@ namespace {
 __device__ __forceinline__ int clamped(int x, int most) { return x < 0 ? 0 : (x > most ? most : x); }
 
 // ---- choice ----------------------------------------------------------------
-// One workgroup per sequence: the totals come from memory once, then from L2 once
-// per digit of the threshold.
+// One workgroup per sequence.
+constexpr int kFewKeys = 8192, kManyKeys = 32768;
+template <int CAPACITY>
 __global__ void __launch_bounds__(choose::kThreads) keep_kernel(const KeepParams p) {
   __shared__ choose::Scratch scratch;
+  __shared__ uint32_t room[CAPACITY];
   const int b = blockIdx.x;
   const int ctx = clamped(p.context_lens[b], p.max_ctx);
   const int first = p.first_tokens ? clamped(p.first_tokens[b], ctx) : 0;
@@ -24,8 +26,8 @@ __global__ void __launch_bounds__(choose::kThreads) keep_kernel(const KeepParams
   for (int i = want + recent + threadIdx.x; i < p.kept_stride; i += choose::kThreads) out[i] = -1;
   if (threadIdx.x == 0) p.kept_lens[b] = want + recent;
   const float* totals = p.totals + (size_t)b * p.totals_stride + first;
-  choose::choose<uint32_t>(n, want, scratch, [&](int i) { return choose::key_of(totals[i]); },
-                           [&](int rank, int i) { out[rank] = i; });
+  choose::choose<uint32_t, CAPACITY>(n, want, scratch, room, [&](int i) { return choose::key_of(totals[i]); },
+                                     [&](int rank, int i) { out[rank] = i; });
 }
 
 // ---- move ------------------------------------------------------------------
@@ -35,8 +37,16 @@ __global__ void __launch_bounds__(choose::kThreads) keep_kernel(const KeepParams
 // round reads lies behind every slot that this one writes (kept ascends, so row j's
 // source is at least slot j), so only the rows of one round can stand in each
 // other's way.  To other blocks the rounds are workgroups of their own (chunks).
-// The rows are read and written once; nothing but their traffic bounds the move.
+//
+// The rows are read and written once; nothing but their traffic bounds the move.  It
+// reads and writes them with the non-temporal hint, and the KV heads run fastest over
+// the workgroups, then the rounds: neighbouring workgroups then move the rows of
+// the same tokens, 256 bytes of each block's neighbouring tiles.  64 sequences of
+// 3001..15000 tokens cut to 4096, 1.5 GB read and written: rounds fastest 640 us, heads
+// fastest 505, with the hint on loads / stores / both 347 / 343 / 337 (4.6 TB/s, a large
+// copy runs at 4.8); one of 30000 cut to 16384 117 / 93 / 89 / 81 (no hint / ...).
 constexpr int kPasses = kMovePasses;
+typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
 
 // The loads before this line have arrived in every thread of the workgroup.
 __device__ __forceinline__ void all_loaded() {
@@ -48,10 +58,10 @@ template <int D>
 __device__ __forceinline__ void move_rows(const CompactParams& p, int wg) {
   constexpr int kRowThreads = D / 8;
   constexpr int kRows = kMoveThreads / kRowThreads;                     // per pass
-  const int chunk = wg % p.chunks;
-  wg /= p.chunks;
   const int g = wg % p.num_kv_heads;
   wg /= p.num_kv_heads;
+  const int chunk = wg % p.chunks;
+  wg /= p.chunks;
   uint16_t* pool = wg & 1 ? p.v_pool : p.k_pool;
   const int b = wg >> 1;
   const int first = p.first_tokens ? clamped(p.first_tokens[b], p.max_ctx) : 0;
@@ -65,7 +75,7 @@ __device__ __forceinline__ void move_rows(const CompactParams& p, int wg) {
     return pool + (((size_t)clamped(id, p.num_blocks - 1) * p.num_kv_heads + g) * 16 + (t & 15)) * D + piece * 8;
   };
   for (int j0 = chunk * kPasses * kRows; j0 < m; j0 += p.chunks * kPasses * kRows) {   // uniform
-    uint4 x[kPasses];
+    u32x4_t x[kPasses];
     uint16_t* dst[kPasses];
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) {
@@ -78,13 +88,13 @@ __device__ __forceinline__ void move_rows(const CompactParams& p, int wg) {
         if (dst[i] == src)
           dst[i] = nullptr;                                             // it stays where it is
         else
-          x[i] = *reinterpret_cast<const uint4*>(src);
+          x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(src));
       }
     }
     all_loaded();
 #pragma unroll
     for (int i = 0; i < kPasses; ++i)
-      if (dst[i]) *reinterpret_cast<uint4*>(dst[i]) = x[i];
+      if (dst[i]) __builtin_nontemporal_store(x[i], reinterpret_cast<u32x4_t*>(dst[i]));
   }
 }
 
@@ -130,7 +140,11 @@ __global__ void __launch_bounds__(kMoveThreads) compact_kernel(const CompactPara
 }  // namespace
 
 hipError_t launch_keep(const KeepParams& p, hipStream_t stream) {
-  hipLaunchKernelGGL(keep_kernel, dim3((unsigned)p.batch), dim3(choose::kThreads), 0, stream, p);
+  const dim3 grid((unsigned)p.batch), wg(choose::kThreads);
+  if (p.max_ctx <= kFewKeys)
+    hipLaunchKernelGGL(keep_kernel<kFewKeys>, grid, wg, 0, stream, p);
+  else
+    hipLaunchKernelGGL(keep_kernel<kManyKeys>, grid, wg, 0, stream, p);
   return hipGetLastError();
 }
 

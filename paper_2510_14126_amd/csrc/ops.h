@@ -119,7 +119,7 @@ hipError_t launch_biased(const BiasedParams& p, hipStream_t stream);
 using BiasedLaunch = hipError_t (*)(const BiasedParams&, hipStream_t);
 hipError_t launch_tree(const BiasedParams& p, hipStream_t stream);
 int biased_size(const pa_kv_pool* pool, int32_t batch, int32_t num_q_heads, int32_t max_context_len,
-                int32_t max_chunk, int32_t window, size_t* bytes_out, const char* fn);
+                int32_t max_chunk, int32_t window, bool tree, size_t* bytes_out, const char* fn);
 int biased_call(const pa_kv_pool* pool, const void* q, const int32_t* q_start, int32_t total_q, const int32_t* parents,
                 const int32_t* block_tables, int32_t bt_stride, const int32_t* context_lens, int32_t batch,
                 int32_t num_q_heads, float scale, float softcap, const float* slopes, int32_t window,

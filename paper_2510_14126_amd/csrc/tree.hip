@@ -27,13 +27,25 @@ tree_big_kernel(const BiasedParams p) {
 }
 
 constexpr int kMergeWaves = 8;
-template <int D, int NW>
+template <int D, int NW, int ROWS>
 __global__ void __launch_bounds__(64 * (NW > 1 ? NW : kWaves)) tree_merge_kernel(const BiasedParams p) {
   __shared__ __attribute__((aligned(16))) float smem[NW > 1 ? NW * (D + 1) : 1];
   const int wave = wave_uniform(threadIdx.x >> 6);
   const int64_t row = NW > 1 ? blockIdx.x : (int64_t)blockIdx.x * kWaves + wave;
   if (row >= (int64_t)p.batch * p.tiles * p.num_kv_heads * p.tile_rows) return;
-  biased::merge_body<D, NW>(p, (int)(row / p.tile_rows), (int)(row % p.tile_rows), NW > 1 ? wave : 0, (lds_f32_t*)smem);
+  biased::merge_body<D, NW, ROWS>(p, (int)(row / p.tile_rows), (int)(row % p.tile_rows), NW > 1 ? wave : 0,
+                                  (lds_f32_t*)smem);
+}
+
+template <int D, int ROWS>
+void launch_merge(const BiasedParams& p, hipStream_t stream) {
+  const int64_t rows = (int64_t)p.batch * p.tiles * p.num_kv_heads * p.tile_rows;
+  if (p.parts > biased::kGroup && rows <= 512)
+    hipLaunchKernelGGL((tree_merge_kernel<D, kMergeWaves, ROWS>), dim3((unsigned)rows), dim3(64 * kMergeWaves), 0, stream,
+                       p);
+  else
+    hipLaunchKernelGGL((tree_merge_kernel<D, 1, ROWS>), dim3((unsigned)((rows + kWaves - 1) / kWaves)), dim3(64 * kWaves),
+                       0, stream, p);
 }
 
 template <int D, bool CAP>
@@ -45,11 +57,10 @@ hipError_t launch_t(const BiasedParams& p, hipStream_t stream) {
   else
     hipLaunchKernelGGL((tree_split_kernel<D, CAP>), grid, wg, 0, stream, p);
   if (p.parts > 1) {
-    const int64_t rows = tiles * p.tile_rows;
-    if (p.parts > biased::kGroup && rows <= 512)
-      hipLaunchKernelGGL((tree_merge_kernel<D, kMergeWaves>), dim3((unsigned)rows), dim3(64 * kMergeWaves), 0, stream, p);
+    if (p.big)
+      launch_merge<D, kBiasedWgRows>(p, stream);
     else
-      hipLaunchKernelGGL((tree_merge_kernel<D, 1>), dim3((unsigned)((rows + kWaves - 1) / kWaves)), wg, 0, stream, p);
+      launch_merge<D, kBiasedTileRows>(p, stream);
   }
   return hipGetLastError();
 }

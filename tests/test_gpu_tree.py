@@ -96,17 +96,19 @@ def test_parents_that_are_none():
 
 
 def test_chain_equals_extend():
-    """A chain is an ordinary chunk: bit for bit what the biased extend gives."""
+    """A chain is an ordinary chunk.  The two calls may take their rows and tokens in other forms, whose sums have other
+    orders: each is within the tolerance of the chunk's oracle, and so they are within twice it of each other."""
     print("[gpu case] tree chain against extend", flush=True)
     c = Tree(5, ctx=[300, 90, 45], chunk=[40, 64, 45], hq=16, hkv=4, d=128, reach=1)
     c.parents[:] = np.concatenate([np.arange(m) - 1 for m in c.chunk])
-    got = c.run()
-    out = torch.zeros_like(c.out)
+    ref = Case.reference(c)
+    c.check(c.run(), ref)
+    out = torch.full_like(c.out, 0x4242)
     ws = torch.zeros(1 << 20, dtype=torch.uint8, device=DEV)
     pa.paged_attn_extend_biased(c.pool, c.t["q"], c.t["start"], c.total, c.t["table"], c.width, c.t["ctx"], 3, 16,
                                 c.scale, 0.0, None, 0, None, None, 300, 64, ws, 1 << 20, out)
     torch.cuda.synchronize()
-    assert np.array_equal(out.cpu().numpy().view(np.uint16), got)
+    c.check(out.cpu().numpy().view(np.uint16), ref)
 
 
 @pytest.mark.parametrize("hq,d", [(8, 128), (8, 64), (64, 128)])
