@@ -140,18 +140,18 @@ __global__ void __launch_bounds__(64 * kWaves) score_kernel(const BlocksParams p
   // the lane's side: pieces of the least values meet the negative parts of q
   const bool upper = piece >= kLanes / 2;
   const uint16_t* q_row = p.q + ((size_t)b * p.num_kv_heads + g) * p.group * D + piece % (kLanes / 2) * 8;
-  uint4 first_row = *reinterpret_cast<const uint4*>(q_row);
+  // 64 table entries at a time, and the 64 behind them; the first before the length is there
+  const int32_t* table = p.block_tables + (size_t)b * p.bt_stride + p.first_blocks;
+  const int most = min(p.key_blocks - p.first_blocks, base + rounds * kPer);
+  auto ids_from = [&](int at) { return at + lane < most ? clamped(table[at + lane], p.num_blocks - 1) : 0; };
+  int ids = ids_from(base), ids_next = ids_from(base + 64);
   const int ctx = clamped(p.context_lens[b], p.max_ctx);
   const int n = candidates(p, (ctx + 15) >> 4);
   const int end = min(n, base + rounds * kPer);
   if (base >= end) return;
-  const int32_t* table = p.block_tables + (size_t)b * p.bt_stride + p.first_blocks;
   const uint16_t* bounds = p.bounds + (size_t)g * (2 * D) + piece * 8;
   const size_t stride = (size_t)p.num_kv_heads * (2 * D);
 
-  // 64 table entries at a time, and the 64 behind them
-  auto ids_from = [&](int at) { return at + lane < end ? clamped(table[at + lane], p.num_blocks - 1) : 0; };
-  int ids = ids_from(base), ids_next = ids_from(base + 64);
   auto load = [&](uint4 (&x)[kLoads], int at) {    // at - base: a multiple of kPer, which divides 64
     if (at > base && ((at - base) & 63) == 0) {
       ids = ids_next;
@@ -167,13 +167,19 @@ __global__ void __launch_bounds__(64 * kWaves) score_kernel(const BlocksParams p
   load(x[0], base);
 
   double q[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-  for (int h = 0; h < p.group; ++h) {
-    const uint4 y = h == 0 ? first_row : *reinterpret_cast<const uint4*>(q_row + (size_t)h * D);
-    const uint32_t w[4] = {y.x, y.y, y.z, y.w};
+  for (int h0 = 0; h0 < p.group; h0 += 4) {
+    uint4 y[4];
 #pragma unroll
-    for (int d = 0; d < 8; ++d) {
-      const float z = d & 1 ? bf16_hi(w[d / 2]) : bf16_lo(w[d / 2]);
-      q[d] += (double)((upper ? z < 0.f : z > 0.f) ? 0.f : z);        // NaN stays
+    for (int k = 0; k < 4; ++k) y[k] = *reinterpret_cast<const uint4*>(q_row + (size_t)min(h0 + k, p.group - 1) * D);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint32_t w[4] = {y[k].x, y[k].y, y[k].z, y[k].w};
+      if (h0 + k < p.group)
+#pragma unroll
+        for (int d = 0; d < 8; ++d) {
+          const float z = d & 1 ? bf16_hi(w[d / 2]) : bf16_lo(w[d / 2]);
+          q[d] += (double)((upper ? z < 0.f : z > 0.f) ? 0.f : z);    // NaN stays
+        }
     }
   }
 
@@ -219,10 +225,10 @@ __global__ void __launch_bounds__(64 * kWaves) score_kernel(const BlocksParams p
 }
 
 // ---- choice ----------------------------------------------------------------
-// One workgroup per (sequence, KV head).
+// One workgroup per (sequence, KV head): of 256 threads up to kFewKeys candidates.
 constexpr int kFewKeys = 2048, kManyKeys = 16384;
-template <int CAPACITY>
-__global__ void __launch_bounds__(choose::kThreads) select_kernel(const BlocksParams p) {
+template <int THREADS, int CAPACITY>
+__global__ void __launch_bounds__(THREADS) select_kernel(const BlocksParams p) {
   __shared__ choose::Scratch scratch;
   __shared__ uint64_t room[CAPACITY];
   const int g = blockIdx.x % p.num_kv_heads, b = blockIdx.x / p.num_kv_heads;
@@ -231,17 +237,18 @@ __global__ void __launch_bounds__(choose::kThreads) select_kernel(const BlocksPa
   const int nblk = (ctx + 15) >> 4;
   int32_t* out = p.selected + row * p.max_blocks;
   const int n = candidates(p, nblk);
-  if (n <= 0) {
-    for (int i = threadIdx.x; i < p.max_blocks; i += choose::kThreads) out[i] = i < nblk ? i : -1;
+  const uint64_t* keys = p.keys + row * p.key_blocks;
+  const int bound = p.key_blocks > p.max_blocks ? p.key_blocks - p.first_blocks - p.last_blocks : 0;
+  const int want = n > 0 ? p.max_blocks - p.first_blocks - p.last_blocks : 0;     // < n
+  choose::choose<uint64_t, THREADS, CAPACITY>(bound, n, want, scratch, room, [&](int i) { return keys[i]; },
+                                              [&](int rank, int i) { out[p.first_blocks + rank] = p.first_blocks + i; });
+  if (n <= 0) {                                                       // all of them (or nothing between first and last)
+    for (int i = threadIdx.x; i < p.max_blocks; i += THREADS) out[i] = i < nblk ? i : -1;
     return;
   }
-  const int want = p.max_blocks - p.first_blocks - p.last_blocks;     // < n
-  for (int i = threadIdx.x; i < p.first_blocks; i += choose::kThreads) out[i] = i;
-  for (int i = threadIdx.x; i < p.last_blocks; i += choose::kThreads)
+  for (int i = threadIdx.x; i < p.first_blocks; i += THREADS) out[i] = i;
+  for (int i = threadIdx.x; i < p.last_blocks; i += THREADS)
     out[p.max_blocks - p.last_blocks + i] = nblk - p.last_blocks + i;
-  const uint64_t* keys = p.keys + row * p.key_blocks;
-  choose::choose<uint64_t, CAPACITY>(n, want, scratch, room, [&](int i) { return keys[i]; },
-                                     [&](int rank, int i) { out[p.first_blocks + rank] = p.first_blocks + i; });
 }
 
 }  // namespace
@@ -269,11 +276,11 @@ hipError_t launch_select(const BlocksParams& p, hipStream_t stream) {
     else
       hipLaunchKernelGGL(score_kernel<64>, grid, wg, 0, stream, p, rounds);
   }
-  const dim3 grid((unsigned)rows), wg(choose::kThreads);
+  const dim3 grid((unsigned)rows);
   if (p.key_blocks - p.first_blocks - p.last_blocks <= kFewKeys)
-    hipLaunchKernelGGL(select_kernel<kFewKeys>, grid, wg, 0, stream, p);
+    hipLaunchKernelGGL((select_kernel<256, kFewKeys>), grid, dim3(256), 0, stream, p);
   else
-    hipLaunchKernelGGL(select_kernel<kManyKeys>, grid, wg, 0, stream, p);
+    hipLaunchKernelGGL((select_kernel<1024, kManyKeys>), grid, dim3(1024), 0, stream, p);
   return hipGetLastError();
 }
 

@@ -1,5 +1,5 @@
-// The `want` largest of n keys, by one workgroup of kChooseThreads: their ranks in
-// the keys' own order.  Equal keys: the first ones.
+// The `want` largest of n keys, by one workgroup: their ranks in the keys' own order.
+// Equal keys: the first ones.
 //
 // The threshold is found from the top: the highest bit in which any two keys differ,
 // then eight bits of it and those below at a time, a histogram in LDS of the keys
@@ -9,6 +9,13 @@
 // be one counter that every thread adds to.)  Then every wavefront counts its
 // stretch of keys above and on the threshold, and writes them behind those of the
 // stretches before.  Nothing depends on the order of the atomics.
+//
+// A short chain bounds it: a handful of passes with a barrier after each.  So the keys
+// wait in LDS; every wavefront reads a digit's histogram for itself, and each digit has
+// one of its own, zeroed beforehand; and of 64-bit keys the passes look at the 32 bits
+// from the first differing one on (the others decide only between keys that are equal
+// in those, and then all digits are gone through).  Unrolled over registers the passes
+// were slower: code that is fetched from L2 as it runs, once.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -19,14 +26,13 @@
 namespace pa {
 namespace choose {
 
-constexpr int kThreads = 1024;
-constexpr int kWavesHere = kThreads / 64;
+constexpr int kMostWaves = 16;
+constexpr int kDigits = 8;                // of a 64-bit key
 
 struct Scratch {
-  uint64_t any[kWavesHere];
-  uint32_t hist[256];
-  int32_t above[kWavesHere], equal[kWavesHere];
-  int32_t digit, need, exact;
+  uint64_t any[kMostWaves];
+  int32_t above[kMostWaves], equal[kMostWaves];
+  alignas(16) uint32_t hist[kDigits][256];
 };
 
 // Keys that order as the values do, NaN above all, -0 as 0.
@@ -41,81 +47,99 @@ __device__ __forceinline__ uint32_t key_of(float x) {
   return u >> 31 ? ~u : u | 0x80000000u;
 }
 
-// load(i): key i < n.  emit(rank, i): key i is one of the chosen, rank < want.  Every
-// thread of the workgroup calls it, with the same n and 0 < want < n.
-template <typename Key, typename Load, typename Emit>
-__device__ __forceinline__ void choose_some(int n, int want, Scratch& s, const Load& load, const Emit& emit) {
+// x >> s for 0 <= s <= the type's bits.
+template <typename T>
+__device__ __forceinline__ T shifted(T x, int s) {
+  return s >= (int)(8 * sizeof(T)) ? (T)0 : (T)(x >> s);
+}
+
+// Sums over this lane and those before it, and the bits of all lanes together: DPP
+// moves within the rows of 16, then each row's last lane to the rows behind it.  (The
+// same through the LDS crossbar was half of a digit's time, sixteen wavefronts at it.)
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint32_t moved(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, ROWS, 0xf, false);
+}
+constexpr int kDppRowShr1 = 0x111, kDppRowBcast15 = 0x142, kDppRowBcast31 = 0x143;
+__device__ __forceinline__ uint32_t sum_before(uint32_t x) {
+  x += moved<kDppRowShr1, 0xf>(x);
+  x += moved<kDppRowShr1 + 1, 0xf>(x);
+  x += moved<kDppRowShr1 + 3, 0xf>(x);
+  x += moved<kDppRowShr1 + 7, 0xf>(x);
+  x += moved<kDppRowBcast15, 0xa>(x);
+  x += moved<kDppRowBcast31, 0xc>(x);
+  return x;
+}
+__device__ __forceinline__ uint32_t any_bits(uint32_t x) {
+  x |= moved<kDppRowShr1, 0xf>(x);
+  x |= moved<kDppRowShr1 + 1, 0xf>(x);
+  x |= moved<kDppRowShr1 + 3, 0xf>(x);
+  x |= moved<kDppRowShr1 + 7, 0xf>(x);
+  x |= moved<kDppRowBcast15, 0xa>(x);
+  x |= moved<kDppRowBcast31, 0xc>(x);
+  return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+}
+
+// Keys of which `bits` bits are undecided, seen as U values of that many bits at most:
+// the threshold's bits from `hi` on (fixed), and how many of the keys that share them
+// are wanted (need).  exact: all of them.
+template <typename U>
+struct Threshold {
+  int hi, need;
+  U fixed;
+  bool exact;
+};
+// each(f): f(key, there) for the lane's keys.
+template <typename U, typename Each>
+__device__ __forceinline__ Threshold<U> threshold(Scratch& s, int bits, int want, const Each& each) {
   const int lane = threadIdx.x & 63;
-  const int wave = wave_uniform(threadIdx.x >> 6);
-  constexpr int kBits = 8 * sizeof(Key);
-  const Key key0 = load(0);
-  // a wavefront's stretch of the keys, whole groups of 64
-  const int stretch = (n + kThreads - 1) / kThreads * 64;
-  const int from = min(n, wave * stretch), to = min(n, from + stretch);
-  // f(i, key, in) for the lane's keys, all lanes together; in: there is a key i
-  auto each = [&](const auto& f) {
-    for (int i0 = from; i0 < to; i0 += 64) f(i0 + lane, i0 + lane < to ? load(i0 + lane) : (Key)0, i0 + lane < to);
-  };
-  uint64_t any = 0;
-  each([&](int, Key k, bool in) { any |= in ? (uint64_t)(k ^ key0) : 0; });
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) any |= __shfl_xor((unsigned long long)any, m);
-  if (lane == 0) s.any[wave] = any;
-  __syncthreads();
-  any = 0;
-#pragma unroll
-  for (int w = 0; w < kWavesHere; ++w) any |= s.any[w];
-  // bits from `hi` on are decided: the threshold's are `fixed`
-  int hi = any == 0 ? 0 : 64 - __builtin_clzll(any);
-  auto top = [&](Key k) { return hi == kBits ? (Key)0 : (Key)(k >> hi); };
-  Key fixed = top(key0);
-  int need = want;
-  bool exact = false;
-  while (hi > 0 && !exact) {
-    const int bits = hi < 8 ? hi : 8;
-    const int lo = hi - bits;
-    if (threadIdx.x < 256) s.hist[threadIdx.x] = 0;
-    __syncthreads();
-    each([&](int, Key k, bool in) {
-      if (in && top(k) == fixed) atomicAdd(&s.hist[(uint32_t)(k >> lo) & ((1u << bits) - 1)], 1u);
+  Threshold<U> t{bits, want, (U)0, false};
+  for (int digit = 0; t.hi > 0 && !t.exact; ++digit) {
+    const int width = t.hi < 8 ? t.hi : 8;
+    const int lo = t.hi - width;
+    uint32_t* hist = s.hist[digit];
+    each([&](U k, bool in) {
+      if (in && shifted(k, t.hi) == t.fixed) atomicAdd(&hist[(uint32_t)(k >> lo) & ((1u << width) - 1)], 1u);
     });
     __syncthreads();
-    if (wave == 0) {
-      // lane: digits 255 - 4 lane down to 252 - 4 lane, and the count of those above
-      int c[4], mine = 0;
+    // lane: digits 255 - 4 lane down to 252 - 4 lane, and the count of those above
+    const uint4 four = *reinterpret_cast<const uint4*>(hist + 252 - 4 * lane);
+    const int c[4] = {(int)four.w, (int)four.z, (int)four.y, (int)four.x};
+    const int mine = c[0] + c[1] + c[2] + c[3];
+    int before = (int)sum_before((uint32_t)mine) - mine;
+    int found = -1, rest = 0, all = 0;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        c[j] = (int)s.hist[255 - 4 * lane - j];
-        mine += c[j];
+    for (int j = 0; j < 4; ++j) {
+      if (before < t.need && t.need <= before + c[j]) {          // one lane, one digit
+        found = 255 - 4 * lane - j;
+        rest = t.need - before;
+        all = c[j];
       }
-      int before = mine;
-#pragma unroll
-      for (int m = 1; m < 64; m <<= 1) {
-        const int x = __shfl_up(before, m);
-        if (lane >= m) before += x;
-      }
-      before -= mine;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        if (before < need && need <= before + c[j]) {          // one lane, one digit
-          s.digit = 255 - 4 * lane - j;
-          s.need = need - before;
-          s.exact = need - before == c[j];
-        }
-        before += c[j];
-      }
+      before += c[j];
     }
-    __syncthreads();
-    fixed = (Key)(hi == kBits ? (Key)0 : (Key)(fixed << bits)) | (Key)s.digit;
-    need = s.need;
-    exact = s.exact != 0;
-    hi = lo;
+    const int who = __builtin_ctzll(__builtin_amdgcn_ballot_w64(found >= 0));
+    t.fixed = (U)(t.fixed << width) | (U)__builtin_amdgcn_readlane(found, who);
+    t.need = __builtin_amdgcn_readlane(rest, who);
+    t.exact = __builtin_amdgcn_readlane(all, who) == t.need;
+    t.hi = lo;
   }
+  return t;
+}
 
+// Lanes of a mask below this one.
+__device__ __forceinline__ int below(uint64_t mask) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
+}
+
+// Writes the chosen keys of the workgroup's stretches.  each(f): f(i, key, there).
+template <typename U, typename Each, typename Emit>
+__device__ __forceinline__ void write_chosen(Scratch& s, const Threshold<U>& t, int wave, const Each& each, const Emit& emit) {
+  const int lane = threadIdx.x & 63;
   int above = 0, equal = 0;
-  each([&](int, Key k, bool in) {
-    above += __builtin_popcountll(__builtin_amdgcn_ballot_w64(in && top(k) > fixed));
-    equal += __builtin_popcountll(__builtin_amdgcn_ballot_w64(in && top(k) == fixed));
+  each([&](int, U k, bool in) {
+    const U x = shifted(k, t.hi);
+    above += __builtin_popcountll(__builtin_amdgcn_ballot_w64(in && x > t.fixed));
+    equal += __builtin_popcountll(__builtin_amdgcn_ballot_w64(in && x == t.fixed));
   });
   if (lane == 0) {
     s.above[wave] = above;
@@ -128,38 +152,98 @@ __device__ __forceinline__ void choose_some(int n, int want, Scratch& s, const L
     above += s.above[w];
     equal += s.equal[w];
   }
-  const uint64_t below = (1ull << lane) - 1;
-  each([&](int i, Key k, bool in) {
-    const Key t = top(k);
-    const uint64_t a = __builtin_amdgcn_ballot_w64(in && t > fixed), e = __builtin_amdgcn_ballot_w64(in && t == fixed);
-    const int a_rank = above + __builtin_popcountll(a & below), e_rank = equal + __builtin_popcountll(e & below);
-    if (in && (t > fixed || (t == fixed && e_rank < need))) emit(a_rank + min(e_rank, need), i);
+  each([&](int i, U k, bool in) {
+    const U x = shifted(k, t.hi);
+    const uint64_t a = __builtin_amdgcn_ballot_w64(in && x > t.fixed), e = __builtin_amdgcn_ballot_w64(in && x == t.fixed);
+    if ((a | e) == 0) return;                                    // uniform
+    const int e_rank = equal + below(e);
+    if (in && (x > t.fixed || (x == t.fixed && e_rank < t.need))) emit(above + below(a) + min(e_rank, t.need), i);
     above += __builtin_popcountll(a);
     equal += __builtin_popcountll(e);
   });
 }
 
-// The same for 0 <= want <= n.  Up to CAPACITY keys wait in LDS (`room`), which takes
-// the passes' loads from L2 out of the chain.
-// (In registers they are slower: the unrolled passes are code that is fetched from L2
-// as it runs, once, 11.7 / 9.3 us for 512 rows of 250..1800 keys.)
-template <typename Key, int CAPACITY, typename Load, typename Emit>
-__device__ __forceinline__ void choose(int n, int want, Scratch& s, Key* room, const Load& load, const Emit& emit) {
+// load(i): key i < bound, of which the first n <= bound count (bound is known before
+// n arrives, and the first loads need not wait for it).  emit(rank, i): key i is one of
+// the chosen, rank < want.  All THREADS of the workgroup call it, with the same n and
+// 0 <= want <= n.  Up to CAPACITY keys wait in `room`; more are loaded anew by each pass.
+template <typename Key, int THREADS, int CAPACITY, typename Load, typename Emit>
+__device__ __forceinline__ void choose(int bound, int n, int want, Scratch& s, Key* room, const Load& load, const Emit& emit) {
+  const int lane = threadIdx.x & 63;
+  const int wave = wave_uniform(threadIdx.x >> 6);
+  constexpr int kFirst = 4;
+  const Key key0 = bound > 0 ? load(0) : (Key)0;
+  Key first[kFirst];
+#pragma unroll
+  for (int k = 0; k < kFirst; ++k) first[k] = (int)threadIdx.x + k * THREADS < bound ? load(threadIdx.x + k * THREADS) : (Key)0;
   if (want <= 0) return;
   if (want >= n) {
-    for (int i = threadIdx.x; i < n; i += kThreads) emit(i, i);
+    for (int i = threadIdx.x; i < n; i += THREADS) emit(i, i);
     return;
   }
-  if (n > CAPACITY) {
-    choose_some<Key>(n, want, s, load, emit);
-    return;
-  }
-  const int stretch = (n + kThreads - 1) / kThreads * 64;
-  const int from = min(n, wave_uniform(threadIdx.x >> 6) * stretch), to = min(n, from + stretch);
+  for (int i = threadIdx.x; i < kDigits * 256; i += THREADS) (&s.hist[0][0])[i] = 0;
+  // a wavefront's stretch of the keys, whole groups of 64
+  const int stretch = (n + THREADS - 1) / THREADS * 64;
+  const int from = min(n, wave * stretch), to = min(n, from + stretch);
+  uint64_t any = 0;
+  const bool held = n <= CAPACITY;
+  auto seen = [&](int i, Key k) {
+    if (held) room[i] = k;
+    any |= (uint64_t)(k ^ key0);
+  };
+#pragma unroll
+  for (int k = 0; k < kFirst; ++k)
+    if ((int)threadIdx.x + k * THREADS < n) seen(threadIdx.x + k * THREADS, first[k]);
 #pragma unroll 4
-  for (int i = from + (threadIdx.x & 63); i < to; i += 64) room[i] = load(i);
+  for (int i = threadIdx.x + kFirst * THREADS; i < n; i += THREADS) seen(i, load(i));
+  any = (uint64_t)any_bits((uint32_t)(any >> 32)) << 32 | any_bits((uint32_t)any);
+  if (lane == 0) s.any[wave] = any;
   __syncthreads();
-  choose_some<Key>(n, want, s, [&](int i) { return room[i]; }, emit);
+  any = 0;
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w) any |= s.any[w];
+  const int bits = any == 0 ? 0 : 64 - __builtin_clzll(any);          // that are not the same in all keys
+
+  auto passes = [&](const auto& key_at) {
+    // the 32 highest of those bits
+    const int drop = max(0, bits - 32);
+    const uint32_t mask = bits - drop >= 32 ? ~0u : (1u << (bits - drop)) - 1;
+    auto each = [&](const auto& f) {
+      Key k = from + lane < to ? key_at(from + lane) : (Key)0;
+      for (int i0 = from; i0 < to; i0 += 64) {
+        const Key next = i0 + 64 + lane < to ? key_at(i0 + 64 + lane) : (Key)0;    // on its way during this one
+        f(i0 + lane, (uint32_t)shifted(k, drop) & mask, i0 + lane < to);
+        k = next;
+      }
+    };
+    const auto t = threshold<uint32_t>(s, bits - drop, want, [&](const auto& f) {
+#pragma unroll 4
+      for (int i = from + lane; i < to; i += 64) f((uint32_t)shifted(key_at(i), drop) & mask, true);
+    });
+    if (t.exact || drop == 0) {
+      write_chosen<uint32_t>(s, t, wave, each, emit);
+      return;
+    }
+    // keys equal in all of those stand on both sides: all bits
+    __syncthreads();
+    for (int i = threadIdx.x; i < kDigits * 256; i += THREADS) (&s.hist[0][0])[i] = 0;
+    __syncthreads();
+    const uint64_t wide = bits >= 64 ? ~0ull : (1ull << bits) - 1;
+    auto each_wide = [&](const auto& f) {
+      for (int i0 = from; i0 < to; i0 += 64) {
+        const bool in = i0 + lane < to;
+        f(i0 + lane, (uint64_t)(in ? key_at(i0 + lane) : (Key)0) & wide, in);
+      }
+    };
+    const auto u = threshold<uint64_t>(s, bits, want, [&](const auto& f) {
+      each_wide([&](int, uint64_t k, bool in) { f(k, in); });
+    });
+    write_chosen<uint64_t>(s, u, wave, each_wide, emit);
+  };
+  if (held)
+    passes([&](int i) { return room[i]; });
+  else
+    passes(load);
 }
 
 }  // namespace choose

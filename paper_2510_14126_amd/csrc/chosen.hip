@@ -10,7 +10,7 @@ using mfma::kWaves;
 template <int D, int GP, bool LISTED, bool WEIGHTS, int AUX>
 __global__ void __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 8)))
 chosen_decode_kernel(const TokensParams p) {
-  __shared__ __attribute__((aligned(16))) uint8_t smem[biased::kDecodeLdsBytes<D, GP>];
+  __shared__ __attribute__((aligned(16))) uint8_t smem[chosen::kChosenLdsBytes<D, GP, WEIGHTS>];
   chosen::decode_body<D, GP, LISTED, WEIGHTS, AUX>(p, blockIdx.x, (lds_u8_t*)smem);
 }
 

@@ -9,10 +9,10 @@ namespace {
 __device__ __forceinline__ int clamped(int x, int most) { return x < 0 ? 0 : (x > most ? most : x); }
 
 // ---- choice ----------------------------------------------------------------
-// One workgroup per sequence.
-constexpr int kFewKeys = 8192, kManyKeys = 32768;
-template <int CAPACITY>
-__global__ void __launch_bounds__(choose::kThreads) keep_kernel(const KeepParams p) {
+// One workgroup per sequence: of 256 threads up to kFewKeys candidates.
+constexpr int kFewKeys = 2048, kManyKeys = 32768;
+template <int THREADS, int CAPACITY>
+__global__ void __launch_bounds__(THREADS) keep_kernel(const KeepParams p) {
   __shared__ choose::Scratch scratch;
   __shared__ uint32_t room[CAPACITY];
   const int b = blockIdx.x;
@@ -22,12 +22,12 @@ __global__ void __launch_bounds__(choose::kThreads) keep_kernel(const KeepParams
   const int n = ctx - first - recent;                                   // candidates
   const int want = min(max(p.keep - first - recent, 0), n);
   int32_t* out = p.kept + (size_t)b * p.kept_stride;
-  for (int i = threadIdx.x; i < recent; i += choose::kThreads) out[want + i] = n + i;
-  for (int i = want + recent + threadIdx.x; i < p.kept_stride; i += choose::kThreads) out[i] = -1;
+  for (int i = threadIdx.x; i < recent; i += THREADS) out[want + i] = n + i;
+  for (int i = want + recent + threadIdx.x; i < p.kept_stride; i += THREADS) out[i] = -1;
   if (threadIdx.x == 0) p.kept_lens[b] = want + recent;
   const float* totals = p.totals + (size_t)b * p.totals_stride + first;
-  choose::choose<uint32_t, CAPACITY>(n, want, scratch, room, [&](int i) { return choose::key_of(totals[i]); },
-                                     [&](int rank, int i) { out[rank] = i; });
+  choose::choose<uint32_t, THREADS, CAPACITY>(p.max_ctx - first, n, want, scratch, room, [&](int i) { return choose::key_of(totals[i]); },
+                                              [&](int rank, int i) { out[rank] = i; });
 }
 
 // ---- move ------------------------------------------------------------------
@@ -140,11 +140,11 @@ __global__ void __launch_bounds__(kMoveThreads) compact_kernel(const CompactPara
 }  // namespace
 
 hipError_t launch_keep(const KeepParams& p, hipStream_t stream) {
-  const dim3 grid((unsigned)p.batch), wg(choose::kThreads);
+  const dim3 grid((unsigned)p.batch);
   if (p.max_ctx <= kFewKeys)
-    hipLaunchKernelGGL(keep_kernel<kFewKeys>, grid, wg, 0, stream, p);
+    hipLaunchKernelGGL((keep_kernel<256, kFewKeys>), grid, dim3(256), 0, stream, p);
   else
-    hipLaunchKernelGGL(keep_kernel<kManyKeys>, grid, wg, 0, stream, p);
+    hipLaunchKernelGGL((keep_kernel<1024, kManyKeys>), grid, dim3(1024), 0, stream, p);
   return hipGetLastError();
 }
 
