@@ -76,9 +76,11 @@ struct Plan {
   size_t bytes() const { return o_bytes + lse_bytes + score_bytes; }
 };
 
-// blocks: bound of a row's; score_tokens: 0, or that many tokens' scores are kept.
-int plan_decode(const pa_kv_pool* pool, int32_t batch, int32_t num_q_heads, int64_t blocks, int64_t score_tokens, Plan* pl,
+// blocks: bound of a row's.  weights: the blocks' scores are kept, and every row's
+// log-sum-exp.
+int plan_decode(const pa_kv_pool* pool, int32_t batch, int32_t num_q_heads, int64_t blocks, bool weights, Plan* pl,
                 const char* fn) {
+  const int64_t score_tokens = weights ? blocks * PA_BLOCK_SIZE : 0;
   const int32_t group = num_q_heads / pool->num_kv_heads;
   pl->tile_heads = group <= 4 ? 4 : 8;
   pl->head_tiles = (group + pl->tile_heads - 1) / pl->tile_heads;
@@ -96,7 +98,7 @@ int plan_decode(const pa_kv_pool* pool, int32_t batch, int32_t num_q_heads, int6
   if (parts > 0x7fffffffLL / rows || score_tokens > kMostBytes / 8 / rows)
     return fail(PA_EINVAL, "%s: grid too large", fn);
   pl->o_bytes = parts > 1 ? (size_t)(pl->tiles * pl->tile_heads * parts) * pool->head_dim * sizeof(float) : 0;
-  pl->lse_bytes = parts > 1 || score_tokens > 0 ? (size_t)(pl->tiles * pl->tile_heads * parts) * sizeof(float) : 0;
+  pl->lse_bytes = parts > 1 || weights ? (size_t)(pl->tiles * pl->tile_heads * parts) * sizeof(float) : 0;
   pl->score_bytes = (size_t)(pl->tiles * pl->tile_heads) * score_tokens * sizeof(float);
   return PA_OK;
 }
@@ -159,15 +161,14 @@ int check_totals(const void* totals, const void* totals_out, int64_t totals_stri
 int plan_weights(const pa_kv_pool* pool, int32_t batch, int32_t num_q_heads, int32_t max_context_len, Plan* pl, const char* fn) {
   int rc = check_batch(pool, batch, max_context_len, fn);
   if (rc || (rc = check_heads(pool, num_q_heads, fn))) return rc;
-  const int64_t blocks = blocks_of(max_context_len);
-  return plan_decode(pool, batch, num_q_heads, blocks, blocks * PA_BLOCK_SIZE, pl, fn);
+  return plan_decode(pool, batch, num_q_heads, blocks_of(max_context_len), true, pl, fn);
 }
 
 int plan_selected(const pa_kv_pool* pool, int32_t batch, int32_t num_q_heads, int32_t max_blocks, Plan* pl, const char* fn) {
   int rc = check_batch(pool, batch, 0, fn);
   if (rc || (rc = check_heads(pool, num_q_heads, fn))) return rc;
   if (max_blocks < 0) return fail(PA_EINVAL, "%s: max_blocks = %d < 0", fn, max_blocks);
-  return plan_decode(pool, batch, num_q_heads, max_blocks, 0, pl, fn);
+  return plan_decode(pool, batch, num_q_heads, max_blocks, false, pl, fn);
 }
 
 int select_bytes(const pa_kv_pool* pool, int32_t batch, int32_t max_context_len, int32_t max_blocks, size_t* bytes,

@@ -348,6 +348,21 @@ def test_weights_without_totals_and_repeated():
         assert np.array_equal(c.after.cpu().numpy(), after) and np.array_equal(c.out.cpu().numpy().view(np.uint16), out)
 
 
+def test_contexts_of_none():
+    """A bound of no tokens at all: zeros, and no total is touched."""
+    print("[gpu case] weights of empty contexts", flush=True)
+    c = Weights(14, ctx=[0, 0, 0], chunk=[1] * 3, hq=8, hkv=2, d=128)
+    out, after = c.go(in_place=True)
+    assert (out == 0).all() and np.array_equal(after, c.before)
+    s = Sparse(15, ctx=[0, 0], hq=8, hkv=2, d=64, first=1, last=2, most=5)
+    t = s.setup()
+    s.bound()
+    s.select()
+    s.attend()
+    torch.cuda.synchronize()
+    assert (t["picked"] == -1).all() and (t["out"] == 0).all() and (t["bounds"] == 0x4242).all()
+
+
 def test_weights_of_special_values():
     """What stands behind the context does not matter; a NaN among the scores shows in the sequence's totals alone."""
     print("[gpu case] weights of special values", flush=True)
