@@ -14,10 +14,12 @@
 // [token][GP] beside the partitions' log-sum-exps, from which weights_body makes the
 // weights; the two are 8 GP bytes a token and KV head of traffic against the 4 D of
 // its K and V, where a second pass over the keys would be 2 D and its products again.
-// A wavefront gathers the scores of its 16 blocks of 64 in LDS and stores them
-// together: stored block by block they held up the tiles' loads, which are counted in
-// one queue with them (128 sequences of 64..8192 tokens, 32 heads over 8: 181 us block
-// by block, STORED_US gathered, 155 without any store).
+// These stores cost more than their bytes (128 sequences of 64..8192 tokens, 32 heads
+// over 8, 782 MB of K and V and 24 MB of scores: 172 us, 150 without the stores), so they
+// are kept down.  A wavefront gathers scores in LDS, up to kRoomBlocks a workgroup; a
+// row whose blocks are one partition of no more than that ends with its log-sum-exps at
+// hand, and what goes to memory is one sum over the tile's heads a token, a fourth or an
+// eighth (164 us; 128 of 64..2000 118 / 106).  The others' scores are stored 64 blocks at a time.
 #pragma once
 
 #include "biased_decode.h"
@@ -53,8 +55,20 @@ __device__ __forceinline__ Place place_of(const TokensParams& p, int wg) {
   return x;
 }
 
-template <int D, int GP> constexpr int kScoreRoom = (kDecodeLdsBytes<D, GP> + 15) / 16 * 16;   // begins here
-template <int GP> constexpr int kScoreBytes = 64 * 16 * GP * 4;                               // of 64 blocks
+// the merge's floats and the rows' log-sum-exps, or the stages, then the scores
+template <int D, int GP>
+constexpr int kScoreRoom = ((2 * kWaves * GP + kWaves * GP * D + GP) * 4 > kDecodeLdsBytes<D, GP>
+                                ? (2 * kWaves * GP + kWaves * GP * D + GP) * 4 : kDecodeLdsBytes<D, GP>) / 16 * 16;
+static_assert(kScoreRoom<64, 4> % 16 == 0 && (2 * kWaves * 4 + kWaves * 4 * 64 + 4) * 4 % 16 == 0, "16-byte records");
+template <int GP> constexpr int kRoomBlocks = GP == 4 ? 128 : 64;    // three workgroups fit a CU
+template <int GP> constexpr int kScoreBytes = kRoomBlocks<GP> * 16 * GP * 4;
+// Whether a sequence's rows keep their scores in LDS (weights): its blocks are one
+// partition, and there is room.
+template <int GP>
+__device__ __forceinline__ bool kept_whole(const TokensParams& p, int nblk) {
+  return nblk <= kRoomBlocks<GP> && nblk <= p.part_blocks;
+}
+template <int D, int GP> constexpr int kLsePlace = 2 * kWaves * GP + kWaves * GP * D;         // floats: behind the merge's
 template <int D, int GP, bool WEIGHTS>
 constexpr int kChosenLdsBytes = WEIGHTS ? kScoreRoom<D, GP> + kScoreBytes<GP> : kDecodeLdsBytes<D, GP>;
 
@@ -99,6 +113,7 @@ __device__ __forceinline__ void decode_body(const TokensParams& p, int wg, lds_u
     return;
   }
   float* scores = WEIGHTS ? p.scores + (size_t)tile_index * p.score_tokens * GP : nullptr;
+  const bool whole = WEIGHTS && kept_whole<GP>(p, nblk);
   lds_f32_t* room = reinterpret_cast<lds_f32_t*>(smem + kScoreRoom<D, GP> + wave * (kScoreBytes<GP> / kWaves));
 
   WaveState<D> S;
@@ -155,7 +170,7 @@ __device__ __forceinline__ void decode_body(const TokensParams& p, int wg, lds_u
             if constexpr (WEIGHTS) {
               // Columns n and n ^ GP (and at GP = 4 all four fours) hold the same scores: each
               // stores another register's, 64 floats side by side per instruction.
-              lds_f32_t* dst = room + i / kWaves * (16 * GP);
+              lds_f32_t* dst = room + ((whole ? c0 : 0) + i) / kWaves * (16 * GP);
               if constexpr (GP == 4) {
                 const int r = n >> 2;
                 const float x = r == 0 ? e[0] : (r == 1 ? e[1] : (r == 2 ? e[2] : e[3]));
@@ -174,7 +189,7 @@ __device__ __forceinline__ void decode_body(const TokensParams& p, int wg, lds_u
         }
       }
     }
-    if constexpr (WEIGHTS) {
+    if (WEIGHTS && !whole) {
       __builtin_amdgcn_wave_barrier();
       constexpr int kLanes = 4 * GP;                    // lanes that hold a block's scores, four each
       for (int k = lane / kLanes; wave + kWaves * k < cn; k += 64 / kLanes) {
@@ -190,9 +205,31 @@ __device__ __forceinline__ void decode_body(const TokensParams& p, int wg, lds_u
       store_partial2(p.part_o + (slot * GP + r) * D + d, o0, o1);
     else
       *reinterpret_cast<uint32_t*>(p.out + ((size_t)at.b * p.num_q_heads + head0 + r) * D + d) = pack_bf16(o0, o1);
-    if (d == 0 && (p.parts > 1 || WEIGHTS))
-      p.part_lse[slot * GP + r] = lt == 0.f ? -__builtin_inff() : mref + log2f(lt);
+    if (d == 0 && (p.parts > 1 || WEIGHTS)) {
+      const float lse = lt == 0.f ? -__builtin_inff() : mref + log2f(lt);
+      p.part_lse[slot * GP + r] = lse;
+      if constexpr (WEIGHTS) reinterpret_cast<lds_f32_t*>(smem)[kLsePlace<D, GP> + r] = lt == 0.f ? __builtin_inff() : lse;
+    }
   });
+  if (WEIGHTS && whole) {
+    __syncthreads();
+    float lse[GP];
+#pragma unroll
+    for (int r = 0; r < GP; ++r) lse[r] = r < rows ? reinterpret_cast<lds_f32_t*>(smem)[kLsePlace<D, GP> + r] : __builtin_inff();
+    const lds_f32_t* all = reinterpret_cast<const lds_f32_t*>(smem + kScoreRoom<D, GP>);
+    for (int t = threadIdx.x; t < ctx; t += 64 * kWaves) {
+      const int j = t >> 4;
+      const lds_f32_t* e = all + (j % kWaves) * (kScoreBytes<GP> / kWaves / 4) + (j / kWaves * 16 + (t & 15)) * GP;
+      float sum = 0.f;
+#pragma unroll
+      for (int r4 = 0; r4 < GP; r4 += 4) {
+        const floatx4_t x = *reinterpret_cast<const mfma::lds_floatx4_t*>(e + r4);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) sum += fast_exp2(x[r] - lse[r4 + r]);
+      }
+      scores[t] = sum;
+    }
+  }
 }
 
 // One row (query head) of a sequence from its partitions: one wavefront, weights
@@ -255,6 +292,15 @@ __device__ __forceinline__ void weights_body(const TokensParams& p, int b, int c
   const int t = chunk * 256 + threadIdx.x;
   if (chunk * 256 >= ctx) return;                       // whole workgroup
   const int planes = p.head_tiles * p.num_kv_heads;     // of GP heads (those past the group's are not read)
+  const size_t at = (size_t)b * p.totals_stride + t;
+  if (kept_whole<GP>(p, (ctx + 15) >> 4)) {                 // a sum per plane and token
+    const float* s = p.scores + (size_t)b * planes * p.score_tokens * GP + min(t, ctx - 1);
+    float sum = 0.f;
+#pragma unroll 8
+    for (int i = 0; i < planes; ++i) sum += s[(size_t)i * p.score_tokens * GP];
+    if (t < ctx) p.totals_out[at] = fmaf(p.decay, p.totals ? p.totals[at] : 0.f, sum);
+    return;
+  }
   const int nparts = p.parts == 1 ? 1 : min(p.parts, ((ctx + 15) / 16 + p.part_blocks - 1) / p.part_blocks);
   const size_t plane0 = (size_t)b * planes;
   float sum = 0.f;
@@ -307,10 +353,7 @@ __device__ __forceinline__ void weights_body(const TokensParams& p, int b, int c
 #pragma unroll
       for (int r = 0; r < GP / 4; ++r) add(i, 4 * r, *reinterpret_cast<const floatx4_t*>(s + i * step + 4 * r));
   }
-  if (t < ctx) {
-    const size_t at = (size_t)b * p.totals_stride + t;
-    p.totals_out[at] = fmaf(p.decay, p.totals ? p.totals[at] : 0.f, sum);
-  }
+  if (t < ctx) p.totals_out[at] = fmaf(p.decay, p.totals ? p.totals[at] : 0.f, sum);
 }
 
 }  // namespace chosen
