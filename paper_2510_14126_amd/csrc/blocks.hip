@@ -81,17 +81,21 @@ __global__ void __launch_bounds__(256) bounds_kernel(const BlocksParams p, int b
 // that of its scalar fp32, and what bounds the pass is reading the bounds, 4 D bytes
 // a block and KV head, a sixteenth of its keys and values.
 //
-// D / 4 lanes read a block's bounds, 16 bytes each; a wavefront has kLoads loads in
+// D / 4 lanes read a block's bounds, 16 bytes each, with the non-temporal hint (the
+// step of 64 sequences below 159 -> 153 us); a wavefront has kLoads loads in
 // flight for its next round while it sums the blocks of this one.  The lanes' partial
 // sums are exchanged so that each step halves the blocks a lane still holds.
 constexpr int kLoads = 8;
 template <int D> constexpr int kGroups = 64 / (D / 4);                // blocks per load
 template <int D> constexpr int kRoundBlocks = kLoads * kGroups<D>;    // blocks per wavefront and round
 constexpr int kWaves = 4;
-// Rounds of a wavefront: as many as leave kFillWaves wavefronts (four times what the
-// GPU holds), so that the chain of loads before a wavefront's first round (length,
-// table, bounds) and its sums of q are paid once for several.
-constexpr int kFillWaves = 16 * 1024, kMostRounds = 16;
+// Rounds of a wavefront: as many as leave the GPU full (kFillWaves), so that the chain
+// of loads before a wavefront's first round (length, table, bounds) and its sums of q
+// are paid once for several, and few, so that the last ones end together.  Whole steps,
+// 64 sequences of 4097..28672 tokens, 32 heads over 8 (14 rounds to fill), with 1 / 2 / 3
+// / 4 / 8 / 11: 174 / 176 / 153 / 154 / 157 / 159 us; 16 of them (3) 64.5 / 59.5 with 2.
+constexpr int kFillWaves = 4 * 1024, kMostRounds = 4;
+typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
 
 template <int CTRL>
 __device__ __forceinline__ double moved(double x) {
@@ -152,7 +156,7 @@ __global__ void __launch_bounds__(64 * kWaves) score_kernel(const BlocksParams p
   const uint16_t* bounds = p.bounds + (size_t)g * (2 * D) + piece * 8;
   const size_t stride = (size_t)p.num_kv_heads * (2 * D);
 
-  auto load = [&](uint4 (&x)[kLoads], int at) {    // at - base: a multiple of kPer, which divides 64
+  auto load = [&](u32x4_t (&x)[kLoads], int at) {    // at - base: a multiple of kPer, which divides 64
     if (at > base && ((at - base) & 63) == 0) {
       ids = ids_next;
       ids_next = ids_from(at + 64);
@@ -160,10 +164,10 @@ __global__ void __launch_bounds__(64 * kWaves) score_kernel(const BlocksParams p
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const size_t id = (size_t)__shfl(ids, ((at - base) & 63) + i * kGroups<D> + part);
-      x[i] = *reinterpret_cast<const uint4*>(bounds + id * stride);
+      x[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(bounds + id * stride));
     }
   };
-  uint4 x[2][kLoads];
+  u32x4_t x[2][kLoads];
   load(x[0], base);
 
   double q[8] = {0, 0, 0, 0, 0, 0, 0, 0};
@@ -184,11 +188,11 @@ __global__ void __launch_bounds__(64 * kWaves) score_kernel(const BlocksParams p
   }
 
   uint64_t* keys = p.keys + ((size_t)b * p.num_kv_heads + g) * p.key_blocks;
-  auto score = [&](const uint4 (&y)[kLoads], int at) {
+  auto score = [&](const u32x4_t (&y)[kLoads], int at) {
     double v[kLoads];
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const uint32_t w[4] = {y[i].x, y[i].y, y[i].z, y[i].w};
+      const uint32_t w[4] = {y[i][0], y[i][1], y[i][2], y[i][3]};
       v[i] = 0.0;
 #pragma unroll
       for (int d = 0; d < 8; ++d) v[i] = fma(q[d], (double)(d & 1 ? bf16_hi(w[d / 2]) : bf16_lo(w[d / 2])), v[i]);
