@@ -129,17 +129,13 @@ __device__ __forceinline__ int candidates(const BlocksParams& p, int nblk) {
   return nblk <= p.max_blocks ? 0 : nblk - p.first_blocks - p.last_blocks;
 }
 
-template <int D>
-__global__ void __launch_bounds__(64 * kWaves) score_kernel(const BlocksParams p, int rounds) {
+// One wavefront's candidates of (sequence b, KV head g), `rounds` rounds from `base` on.
+// store(i, key): candidate i.
+template <int D, typename Store>
+__device__ __forceinline__ void score_blocks(const BlocksParams& p, int b, int g, int base, int rounds, const Store& store) {
   constexpr int kLanes = D / 4;                    // lanes per block
   constexpr int kPer = kRoundBlocks<D>;
   const int lane = threadIdx.x & 63;
-  const int wave = wave_uniform(threadIdx.x >> 6);
-  int wg = blockIdx.x;
-  const int g = wg % p.num_kv_heads;
-  wg /= p.num_kv_heads;
-  const int b = wg % p.batch;
-  const int base = (wg / p.batch * kWaves + wave) * rounds * kPer;
   const int part = lane / kLanes, piece = lane % kLanes;
   // the lane's side: pieces of the least values meet the negative parts of q
   const bool upper = piece >= kLanes / 2;
@@ -187,7 +183,6 @@ __global__ void __launch_bounds__(64 * kWaves) score_kernel(const BlocksParams p
     }
   }
 
-  uint64_t* keys = p.keys + ((size_t)b * p.num_kv_heads + g) * p.key_blocks;
   auto score = [&](const u32x4_t (&y)[kLoads], int at) {
     double v[kLoads];
 #pragma unroll
@@ -217,7 +212,7 @@ __global__ void __launch_bounds__(64 * kWaves) score_kernel(const BlocksParams p
     }
     v[0] += moved<kDppQuadXor1>(v[0]);
     const int block = at + i * kGroups<D> + part;
-    if (block < end && lane % (kLanes / kLoads) == 0) keys[block] = choose::key_of(v[0]);
+    if (block < end && lane % (kLanes / kLoads) == 0) store(block, choose::key_of(v[0]));
   };
   for (int at = base; at < end; at += 2 * kPer) {
     if (at + kPer < end) load(x[1], at + kPer);    // uniform
@@ -228,23 +223,38 @@ __global__ void __launch_bounds__(64 * kWaves) score_kernel(const BlocksParams p
   }
 }
 
+template <int D>
+__global__ void __launch_bounds__(64 * kWaves) score_kernel(const BlocksParams p, int rounds) {
+  const int wave = wave_uniform(threadIdx.x >> 6);
+  int wg = blockIdx.x;
+  const int g = wg % p.num_kv_heads;
+  wg /= p.num_kv_heads;
+  const int b = wg % p.batch;
+  uint64_t* keys = p.keys + ((size_t)b * p.num_kv_heads + g) * p.key_blocks;
+  score_blocks<D>(p, b, g, (wg / p.batch * kWaves + wave) * rounds * kRoundBlocks<D>, rounds,
+                  [&](int i, uint64_t key) { keys[i] = key; });
+}
+
 // ---- choice ----------------------------------------------------------------
 // One workgroup per (sequence, KV head): of 256 threads up to kFewKeys candidates.
+//
+// Up to kFewKeys it can make the keys itself: a launch less, no keys through memory, and
+// while some workgroups choose others still read, but four wavefronts to a row.  It does
+// where the rows fill the GPU (kManyRows), or the candidates are few (kOwnRounds of each
+// wavefront).  Whole steps, 32 heads over 8,
+// scores in a launch of their own / here: one sequence of 64 / 128 / 256 / 500 blocks
+// 17.7 / 15.8, 18.3 / 17.2, 18.8 / 19.3, 19.5 / 24.0 us, four of 128 / 256 19.2 / 17.9,
+// 19.6 / 19.9; 32 (256 rows) of 500 / 2000 32.2 / 30.9, 70.3 / 67.0; 128 of 500 / 1000 /
+// 2000 82.8 / 75.4, 130.7 / 115, 228 / 195.
 constexpr int kFewKeys = 2048, kManyKeys = 16384;
-template <int THREADS, int CAPACITY>
-__global__ void __launch_bounds__(THREADS) select_kernel(const BlocksParams p) {
-  __shared__ choose::Scratch scratch;
-  __shared__ uint64_t room[CAPACITY];
-  const int g = blockIdx.x % p.num_kv_heads, b = blockIdx.x / p.num_kv_heads;
-  const size_t row = (size_t)b * p.num_kv_heads + g;
-  const int ctx = clamped(p.context_lens[b], p.max_ctx);
-  const int nblk = (ctx + 15) >> 4;
-  int32_t* out = p.selected + row * p.max_blocks;
-  const int n = candidates(p, nblk);
-  const uint64_t* keys = p.keys + row * p.key_blocks;
+constexpr int kOwnRounds = 3, kManyRows = 256;
+template <int THREADS, int CAPACITY, typename Keys>
+__device__ __forceinline__ void select_row(const BlocksParams& p, int b, int g, int n, int nblk, choose::Scratch& scratch,
+                                           uint64_t* room, const Keys& keys) {
+  int32_t* out = p.selected + ((size_t)b * p.num_kv_heads + g) * p.max_blocks;
   const int bound = p.key_blocks > p.max_blocks ? p.key_blocks - p.first_blocks - p.last_blocks : 0;
   const int want = n > 0 ? p.max_blocks - p.first_blocks - p.last_blocks : 0;     // < n
-  choose::choose<uint64_t, THREADS, CAPACITY>(bound, n, want, scratch, room, [&](int i) { return keys[i]; },
+  choose::choose<uint64_t, THREADS, CAPACITY>(bound, n, want, scratch, room, keys,
                                               [&](int rank, int i) { out[p.first_blocks + rank] = p.first_blocks + i; });
   if (n <= 0) {                                                       // all of them (or nothing between first and last)
     for (int i = threadIdx.x; i < p.max_blocks; i += THREADS) out[i] = i < nblk ? i : -1;
@@ -253,6 +263,28 @@ __global__ void __launch_bounds__(THREADS) select_kernel(const BlocksParams p) {
   for (int i = threadIdx.x; i < p.first_blocks; i += THREADS) out[i] = i;
   for (int i = threadIdx.x; i < p.last_blocks; i += THREADS)
     out[p.max_blocks - p.last_blocks + i] = nblk - p.last_blocks + i;
+}
+
+template <int D>
+__global__ void __launch_bounds__(64 * kWaves) select_own_kernel(const BlocksParams p, int rounds) {
+  __shared__ choose::Scratch scratch;
+  __shared__ uint64_t room[kFewKeys];
+  const int g = blockIdx.x % p.num_kv_heads, b = blockIdx.x / p.num_kv_heads;
+  const int wave = wave_uniform(threadIdx.x >> 6);
+  score_blocks<D>(p, b, g, wave * rounds * kRoundBlocks<D>, rounds, [&](int i, uint64_t key) { room[i] = key; });
+  const int nblk = (clamped(p.context_lens[b], p.max_ctx) + 15) >> 4;
+  __syncthreads();
+  select_row<64 * kWaves, kFewKeys>(p, b, g, candidates(p, nblk), nblk, scratch, room, [&](int i) { return room[i]; });
+}
+
+template <int THREADS, int CAPACITY>
+__global__ void __launch_bounds__(THREADS) select_kernel(const BlocksParams p) {
+  __shared__ choose::Scratch scratch;
+  __shared__ uint64_t room[CAPACITY];
+  const int g = blockIdx.x % p.num_kv_heads, b = blockIdx.x / p.num_kv_heads;
+  const uint64_t* keys = p.keys + ((size_t)b * p.num_kv_heads + g) * p.key_blocks;
+  const int nblk = (clamped(p.context_lens[b], p.max_ctx) + 15) >> 4;
+  select_row<THREADS, CAPACITY>(p, b, g, candidates(p, nblk), nblk, scratch, room, [&](int i) { return keys[i]; });
 }
 
 }  // namespace
@@ -270,21 +302,30 @@ hipError_t launch_bounds(const BlocksParams& p, hipStream_t stream) {
 
 hipError_t launch_select(const BlocksParams& p, hipStream_t stream) {
   const int64_t rows = (int64_t)p.batch * p.num_kv_heads;
-  if (p.key_blocks > p.max_blocks) {                   // else every sequence attends to all of its blocks
-    const int per = p.head_dim == 128 ? kRoundBlocks<128> : kRoundBlocks<64>;
-    const int64_t n = (p.key_blocks - p.first_blocks - p.last_blocks + per - 1) / per;      // rounds of a row
-    const int rounds = (int)std::min<int64_t>(kMostRounds, std::max<int64_t>(1, rows * n / kFillWaves));
-    const dim3 grid((unsigned)(rows * ((n + kWaves * rounds - 1) / (kWaves * rounds)))), wg(64 * kWaves);
+  const int n = p.key_blocks > p.max_blocks ? p.key_blocks - p.first_blocks - p.last_blocks : 0;   // candidates at most
+  const int per = p.head_dim == 128 ? kRoundBlocks<128> : kRoundBlocks<64>;
+  const int n_rounds = (n + per - 1) / per;
+  const dim3 all((unsigned)rows), wg(64 * kWaves);
+  const int rounds_here = (n_rounds + kWaves - 1) / kWaves;
+  if (n > 0 && n <= kFewKeys && (rounds_here <= kOwnRounds || rows >= kManyRows)) {
+    if (p.head_dim == 128)
+      hipLaunchKernelGGL(select_own_kernel<128>, all, wg, 0, stream, p, rounds_here);
+    else
+      hipLaunchKernelGGL(select_own_kernel<64>, all, wg, 0, stream, p, rounds_here);
+    return hipGetLastError();
+  }
+  if (n > 0) {
+    const int rounds = (int)std::min<int64_t>(kMostRounds, std::max<int64_t>(1, rows * n_rounds / kFillWaves));
+    const dim3 grid((unsigned)(rows * ((n_rounds + kWaves * rounds - 1) / (kWaves * rounds))));
     if (p.head_dim == 128)
       hipLaunchKernelGGL(score_kernel<128>, grid, wg, 0, stream, p, rounds);
     else
       hipLaunchKernelGGL(score_kernel<64>, grid, wg, 0, stream, p, rounds);
   }
-  const dim3 grid((unsigned)rows);
-  if (p.key_blocks - p.first_blocks - p.last_blocks <= kFewKeys)
-    hipLaunchKernelGGL((select_kernel<256, kFewKeys>), grid, dim3(256), 0, stream, p);
+  if (n <= kFewKeys)
+    hipLaunchKernelGGL((select_kernel<256, kFewKeys>), all, dim3(256), 0, stream, p);
   else
-    hipLaunchKernelGGL((select_kernel<1024, kManyKeys>), grid, dim3(1024), 0, stream, p);
+    hipLaunchKernelGGL((select_kernel<1024, kManyKeys>), all, dim3(1024), 0, stream, p);
   return hipGetLastError();
 }
 
