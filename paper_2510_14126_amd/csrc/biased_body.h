@@ -1013,8 +1013,12 @@ __device__ __forceinline__ void big_body(const BiasedParams& p, int wg, lds_u8_t
         publish(s + 2, (u + 2) % kSlots);
         load(s + 3);
         if (busy) {
+          // trees: at raised priority, so that the SIMD's other wavefront publishes and loads
+          // beside the products (64 trees of 13..32 nodes over 2300 tokens 118 -> 115 us)
+          if constexpr (TREE) __builtin_amdgcn_s_setprio(1);
           raw = C.scores(smem + (u + 1) % kSlots * kStageBytes<D>, h, n, query);
           C.attend(a, smem + u * kStageBytes<D>, lane);
+          if constexpr (TREE) __builtin_amdgcn_s_setprio(0);
           a = C.shape(p, raw, first_of(s + 1), h);
           if (s + 1 < nstage) {
             C.reshape(p, a, raw, first_of(s + 1), edge(s + 1), linear(s + 1), h);
