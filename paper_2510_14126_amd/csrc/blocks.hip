@@ -245,9 +245,12 @@ __global__ void __launch_bounds__(64 * kWaves) score_kernel(const BlocksParams p
 // scores in a launch of their own / here: one sequence of 64 / 128 / 256 / 500 blocks
 // 17.7 / 15.8, 18.3 / 17.2, 18.8 / 19.3, 19.5 / 24.0 us, four of 128 / 256 19.2 / 17.9,
 // 19.6 / 19.9; 32 (256 rows) of 500 / 2000 32.2 / 30.9, 70.3 / 67.0; 128 of 500 / 1000 /
-// 2000 82.8 / 75.4, 130.7 / 115, 228 / 195.
+// 2000 82.8 / 75.4, 130.7 / 115, 228 / 195.  Eight wavefronts to a row from kLongRounds
+// rounds on (four / eight: 32 of 500 / 1000 / 2000 31.0 / 30.3, 43.4 / 41.1, 67.3 / 62.8;
+// 128 of 256 / 500 / 1000 / 2000 55.2 / 60.3, 75.4 / 77.4, 115.5 / 115.9, 195 / 193.5; 32 of
+// 125..2000 58.1 / 49.7).
 constexpr int kFewKeys = 2048, kManyKeys = 16384;
-constexpr int kOwnRounds = 3, kManyRows = 256;
+constexpr int kOwnRounds = 3, kManyRows = 256, kLongRounds = 33;
 template <int THREADS, int CAPACITY, typename Keys>
 __device__ __forceinline__ void select_row(const BlocksParams& p, int b, int g, int n, int nblk, choose::Scratch& scratch,
                                            uint64_t* room, const Keys& keys) {
@@ -265,8 +268,8 @@ __device__ __forceinline__ void select_row(const BlocksParams& p, int b, int g, 
     out[p.max_blocks - p.last_blocks + i] = nblk - p.last_blocks + i;
 }
 
-template <int D>
-__global__ void __launch_bounds__(64 * kWaves) select_own_kernel(const BlocksParams p, int rounds) {
+template <int D, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES) select_own_kernel(const BlocksParams p, int rounds) {
   __shared__ choose::Scratch scratch;
   __shared__ uint64_t room[kFewKeys];
   const int g = blockIdx.x % p.num_kv_heads, b = blockIdx.x / p.num_kv_heads;
@@ -274,7 +277,7 @@ __global__ void __launch_bounds__(64 * kWaves) select_own_kernel(const BlocksPar
   score_blocks<D>(p, b, g, wave * rounds * kRoundBlocks<D>, rounds, [&](int i, uint64_t key) { room[i] = key; });
   const int nblk = (clamped(p.context_lens[b], p.max_ctx) + 15) >> 4;
   __syncthreads();
-  select_row<64 * kWaves, kFewKeys>(p, b, g, candidates(p, nblk), nblk, scratch, room, [&](int i) { return room[i]; });
+  select_row<64 * WAVES, kFewKeys>(p, b, g, candidates(p, nblk), nblk, scratch, room, [&](int i) { return room[i]; });
 }
 
 template <int THREADS, int CAPACITY>
@@ -306,12 +309,14 @@ hipError_t launch_select(const BlocksParams& p, hipStream_t stream) {
   const int per = p.head_dim == 128 ? kRoundBlocks<128> : kRoundBlocks<64>;
   const int n_rounds = (n + per - 1) / per;
   const dim3 all((unsigned)rows), wg(64 * kWaves);
-  const int rounds_here = (n_rounds + kWaves - 1) / kWaves;
-  if (n > 0 && n <= kFewKeys && (rounds_here <= kOwnRounds || rows >= kManyRows)) {
-    if (p.head_dim == 128)
-      hipLaunchKernelGGL(select_own_kernel<128>, all, wg, 0, stream, p, rounds_here);
+  if (n > 0 && n <= kFewKeys && (n_rounds <= kOwnRounds * kWaves || rows >= kManyRows)) {
+    auto go = [&](auto kernel, int waves) {
+      hipLaunchKernelGGL(kernel, all, dim3(64 * waves), 0, stream, p, (n_rounds + waves - 1) / waves);
+    };
+    if (n_rounds >= kLongRounds)
+      go(p.head_dim == 128 ? select_own_kernel<128, 8> : select_own_kernel<64, 8>, 8);
     else
-      hipLaunchKernelGGL(select_own_kernel<64>, all, wg, 0, stream, p, rounds_here);
+      go(p.head_dim == 128 ? select_own_kernel<128, 4> : select_own_kernel<64, 4>, 4);
     return hipGetLastError();
   }
   if (n > 0) {

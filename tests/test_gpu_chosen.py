@@ -110,6 +110,8 @@ SPARSE = {
     "long": dict(ctx=[30000, 9001], hq=8, hkv=2, d=64, first=1, last=4, most=150),
     "very_long": dict(ctx=[70001], hq=4, hkv=1, d=64, first=4, last=16, most=256),
     "negative_scale": dict(ctx=[700], hq=8, hkv=2, d=128, first=0, last=1, most=9, scale=-0.1),
+    "many_rows": dict(ctx=[30 + 61 * i for i in range(65)], hq=8, hkv=4, d=64, first=0, last=1, most=10),
+    "many_long_rows": dict(ctx=[5 + 141 * i for i in range(65)], hq=8, hkv=4, d=128, first=1, last=1, most=30),
 }
 
 
@@ -170,6 +172,7 @@ def test_bounds_of_special_keys():
     c = Sparse(6, ctx=[20], hq=4, hkv=1, d=64, first=0, last=1, most=2)
     c.k[c.table[0, 0], 0, 3, 5] = NAN
     c.k[c.table[0, 0], 0, 4, 6] = INF
+    c.k[c.table[0, 0], 0, 5, 8], c.k[c.table[0, 0], 0, 6, 9] = 0x7F81, 0xFF81     # signalling ones
     c.k[c.table[0, 0], 0, :, 7] = NAN
     t = c.setup()
     c.bound()
@@ -177,6 +180,44 @@ def test_bounds_of_special_keys():
     got = bf16_to_f64(t["bounds"].cpu().numpy().view(np.uint16)[c.table[0, 0], 0])
     ref = oracle.block_bounds(bf16_to_f64(c.k[c.table[0, 0], 0]))
     assert np.array_equal(got, ref) and got[0, 7] == np.inf and got[1, 7] == -np.inf and got[1, 6] == np.inf
+
+
+@pytest.mark.parametrize("hkv,d,ctx,most", [(64, 64, 70001, 99), (32, 128, 70001, 2500), (300, 64, 33000, 200), (2, 64, 300000, 64)])
+def test_choice_among_many(hkv, d, ctx, most):
+    """Rounds of several per wavefront, choices beyond the keys that LDS holds: against sorted 64-bit scores (exact inputs)."""
+    print(f"[gpu case] choice among many {hkv} {d} {ctx}", flush=True)
+    gen = torch.Generator(device=DEV).manual_seed(5)
+    nb, group = (ctx + 15) // 16, 2
+    table = torch.randperm(nb, generator=gen, device=DEV)
+    bounds = torch.randint(-127, 128, (nb, hkv, 2, d), generator=gen, device=DEV).float().div_(16).to(torch.bfloat16)
+    bounds = torch.stack([bounds.amin(2), bounds.amax(2)], 2)
+    q = torch.randint(-127, 128, (1, hkv * group, d), generator=gen, device=DEV).float().div_(16).to(torch.bfloat16)
+    scores = torch.zeros((hkv, nb), dtype=torch.float64, device=DEV)
+    for g in range(hkv):
+        lo, hi = (bounds[table, g, i].double() for i in range(2))
+        for h in range(group):
+            x = q[0, g * group + h].double()
+            scores[g] += torch.maximum(x * lo, x * hi).sum(1)
+    first, last = 3, 5
+    order = torch.sort(scores[:, first:nb - last], dim=1, descending=True, stable=True).indices[:, :most - first - last] + first
+    want = torch.cat([torch.arange(first, device=DEV).expand(hkv, -1), torch.sort(order, dim=1).values,
+                      torch.arange(nb - last, nb, device=DEV).expand(hkv, -1)], 1)
+    k = torch.zeros(16, dtype=torch.int16, device=DEV)         # the choice reads no key
+    pool = pa.kv_pool_create(nb, 16, min(hkv, 64), d, k, k)
+    if hkv > 64:                                               # rows by sequences instead: 64 heads are a pool's most
+        batch, heads = hkv // 50, 50
+        pool = pa.kv_pool_create(nb * batch, 16, heads, d, k, k)
+        shuffled = bounds.view(nb, batch, heads, 2, d).transpose(0, 1).reshape(batch * nb, heads, 2, d).contiguous()
+        tables = torch.stack([table + b * nb for b in range(batch)]).int()
+    else:
+        batch, heads, shuffled, tables = 1, hkv, bounds, table.int()[None]
+    size = pa.paged_attn_select_workspace_size(pool, batch, ctx, most)
+    ws = torch.empty(size, dtype=torch.uint8, device=DEV)
+    picked = torch.zeros((batch, heads, most), dtype=torch.int32, device=DEV)
+    pa.paged_attn_select_blocks(pool, q, shuffled, tables.contiguous(), nb, dev32([ctx] * batch), batch, heads * group, ctx,
+                                first, last, most, ws, size, picked)
+    torch.cuda.synchronize()
+    assert torch.equal(picked.view(hkv, most), want.int())
 
 
 @pytest.mark.parametrize("d", [64, 128])
