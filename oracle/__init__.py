@@ -6,7 +6,9 @@ may import this package.  It shares no code with the HIP path.
 Modules: ``attention`` (fp64 numpy oracle, split partials and their merge),
 ``brute`` (pure-Python fsum brute force), ``gate`` (parity tolerance),
 ``kvcache`` (appending a decode step's K/V to the paged cache), ``extend``
-(causal attention of a chunk of new tokens over the paged cache).
+(causal attention of a chunk of new tokens over the paged cache), ``ops``
+(rotated rows, capped, biased and masked attention), ``tokens`` (draft trees,
+chosen blocks, weights per token, kept tokens and their move).
 Every function is pinned by the CPU tests against closed forms, invariants,
 brute force and hand-derived golden values; no function is parity-unpinned.
 """
