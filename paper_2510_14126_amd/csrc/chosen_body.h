@@ -293,12 +293,13 @@ __device__ __forceinline__ void weights_body(const TokensParams& p, int b, int c
   if (chunk * 256 >= ctx) return;                       // whole workgroup
   const int planes = p.head_tiles * p.num_kv_heads;     // of GP heads (those past the group's are not read)
   const size_t at = (size_t)b * p.totals_stride + t;
+  const float before = p.totals && t < ctx ? p.totals[at] : 0.f;
   if (kept_whole<GP>(p, (ctx + 15) >> 4)) {                 // a sum per plane and token
     const float* s = p.scores + (size_t)b * planes * p.score_tokens * GP + min(t, ctx - 1);
     float sum = 0.f;
 #pragma unroll 8
     for (int i = 0; i < planes; ++i) sum += s[(size_t)i * p.score_tokens * GP];
-    if (t < ctx) p.totals_out[at] = fmaf(p.decay, p.totals ? p.totals[at] : 0.f, sum);
+    if (t < ctx) p.totals_out[at] = fmaf(p.decay, before, sum);
     return;
   }
   const int nparts = p.parts == 1 ? 1 : min(p.parts, ((ctx + 15) / 16 + p.part_blocks - 1) / p.part_blocks);
@@ -353,7 +354,7 @@ __device__ __forceinline__ void weights_body(const TokensParams& p, int b, int c
 #pragma unroll
       for (int r = 0; r < GP / 4; ++r) add(i, 4 * r, *reinterpret_cast<const floatx4_t*>(s + i * step + 4 * r));
   }
-  if (t < ctx) p.totals_out[at] = fmaf(p.decay, p.totals ? p.totals[at] : 0.f, sum);
+  if (t < ctx) p.totals_out[at] = fmaf(p.decay, before, sum);
 }
 
 }  // namespace chosen

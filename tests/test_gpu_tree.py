@@ -84,6 +84,23 @@ def test_tree(name, spare):
     c.check(c.run(spare=spare), None, 40.0 * kw.get("qscale", 1.0))
 
 
+@pytest.mark.parametrize("name", ["one_node", "ragged", "cap_64", "many", "long", "long_64", "big_group"])
+def test_small_trees_under_a_large_bound(name):
+    """max_nodes far above the trees: most tiles of the plan, and most rows of the others, are empty."""
+    print(f"[gpu case] tree under 256 nodes {name}", flush=True)
+    c = Tree(len(name) + 60, **TREES[name])
+    c.check(c.run(nodes=256))
+    c.check(c.run(nodes=256, spare=30000))
+
+
+def test_sequences_that_share_blocks():
+    """Trees over a context whose blocks several tables hold."""
+    print("[gpu case] tree over shared blocks", flush=True)
+    c = Tree(21, ctx=[300, 290, 305], chunk=[20, 9, 31], hq=32, hkv=8, d=128, parents=None)
+    c.table[1:, :16] = c.table[0, :16]
+    c.check(c.run())
+
+
 def test_parents_that_are_none():
     """A parent at or behind its node, or negative, stands for the context."""
     print("[gpu case] tree bad parents", flush=True)
