@@ -59,7 +59,8 @@ int paged_attn_tree_workspace_size(const pa_kv_pool *pool, int32_t batch, int32_
  *   num_q_heads      any multiple of the pool's num_kv_heads
  *   softcap          0 (none) or positive, as in paged_attn_decode_biased
  *   max_context_len  below 2^30
- *   max_nodes        bound of L_b, 0 .. PA_TREE_MAX_NODES (more: PA_EUNSUPPORTED)
+ *   max_nodes        bound of L_b, 0 .. PA_TREE_MAX_NODES (more: PA_EUNSUPPORTED), at
+ *                    most max_context_len (or 1)
  *   workspace        device, 16-byte aligned, of workspace_bytes, at least
  *                    paged_attn_tree_workspace_size; its content is not kept.
  *                    Calls that may run at the same time need one each
@@ -79,13 +80,16 @@ int paged_attn_extend_tree(const pa_kv_pool *pool, const void *q, const int32_t 
  *     bounds[block][g][0][d] = min K,   bounds[block][g][1][d] = max K,
  * bf16 [num_blocks][num_kv_heads][2][head_dim], beside the pools (so shared
  * blocks share them).  No key of block j can score higher for query head h than
- * sum_d max(q_hd lo_d, q_hd hi_d); the sum of that over the heads of a KV head
- * is the block's score, and each (sequence, KV head) attends to
+ * sum_d max(q_hd lo_d, q_hd hi_d), that is q_hd hi_d where q_hd >= 0 and q_hd lo_d
+ * elsewhere; the sum of that over the heads of a KV head is the block's score, and
+ * each (sequence, KV head) attends to
  *     its first_blocks first and last_blocks last blocks, and the blocks of the
  *     highest scores among the others, max_blocks in all
  * or to all where it has no more.  Scores are 64-bit sums and equal ones go to
  * the lower block, so the choice is the exact one.  A score of NaN counts as the
- * highest.  (With a negative scale the bound would be the other end's.)
+ * highest.  A dimension that holds NaN in every token of a block bounds nothing: lo is
+ * +infinity and hi -infinity there, and the block's score -infinity (or NaN).  (With a
+ * negative scale the bound would be the other end's.)
  * ------------------------------------------------------------------------- */
 
 /* Bounds of the blocks that hold the tokens first_tokens[b] .. n_b - 1, of the

@@ -241,10 +241,9 @@ __global__ void __launch_bounds__(64 * kWaves) score_kernel(const BlocksParams p
 // Up to kFewKeys it can make the keys itself: a launch less, no keys through memory, and
 // while some workgroups choose others still read, but four wavefronts to a row.  It does
 // where the rows fill the GPU (kManyRows), or the candidates are few (kOwnRounds of each
-// wavefront).  Whole steps, 32 heads over 8,
-// scores in a launch of their own / here: one sequence of 64 / 128 / 256 / 500 blocks
-// 17.7 / 15.8, 18.3 / 17.2, 18.8 / 19.3, 19.5 / 24.0 us, four of 128 / 256 19.2 / 17.9,
-// 19.6 / 19.9; 32 (256 rows) of 500 / 2000 32.2 / 30.9, 70.3 / 67.0; 128 of 500 / 1000 /
+// wavefront).  Whole steps, 32 heads over 8, scores in a launch of their own / here: one
+// sequence of 64 / 128 / 256 / 500 blocks 17.7 / 15.8, 18.3 / 17.2, 18.8 / 19.3, 19.5 /
+// 24.0 us, four of 128 / 256 19.2 / 17.9, 19.6 / 19.9; 32 (256 rows) of 500 / 2000 32.2 / 30.9, 70.3 / 67.0; 128 of 500 / 1000 /
 // 2000 82.8 / 75.4, 130.7 / 115, 228 / 195.  Eight wavefronts to a row from kLongRounds
 // rounds on (four / eight: 32 of 500 / 1000 / 2000 31.0 / 30.3, 43.4 / 41.1, 67.3 / 62.8;
 // 128 of 256 / 500 / 1000 / 2000 55.2 / 60.3, 75.4 / 77.4, 115.5 / 115.9, 195 / 193.5; 32 of
@@ -259,7 +258,7 @@ __device__ __forceinline__ void select_row(const BlocksParams& p, int b, int g, 
   const int want = n > 0 ? p.max_blocks - p.first_blocks - p.last_blocks : 0;     // < n
   choose::choose<uint64_t, THREADS, CAPACITY>(bound, n, want, scratch, room, keys,
                                               [&](int rank, int i) { out[p.first_blocks + rank] = p.first_blocks + i; });
-  if (n <= 0) {                                                       // all of them (or nothing between first and last)
+  if (n <= 0) {                                                       // all of them
     for (int i = threadIdx.x; i < p.max_blocks; i += THREADS) out[i] = i < nblk ? i : -1;
     return;
   }

@@ -55,11 +55,12 @@ __device__ __forceinline__ Place place_of(const TokensParams& p, int wg) {
   return x;
 }
 
-// the merge's floats and the rows' log-sum-exps, or the stages, then the scores
+// The scores' place in LDS: behind the stages, and the merge's floats with the rows'
+// log-sum-exps, which take their room (GP is a multiple of 4: whole 16 bytes).
 template <int D, int GP>
 constexpr int kScoreRoom = ((2 * kWaves * GP + kWaves * GP * D + GP) * 4 > kDecodeLdsBytes<D, GP>
-                                ? (2 * kWaves * GP + kWaves * GP * D + GP) * 4 : kDecodeLdsBytes<D, GP>) / 16 * 16;
-static_assert(kScoreRoom<64, 4> % 16 == 0 && (2 * kWaves * 4 + kWaves * 4 * 64 + 4) * 4 % 16 == 0, "16-byte records");
+                                ? (2 * kWaves * GP + kWaves * GP * D + GP) * 4 : kDecodeLdsBytes<D, GP>);
+static_assert((kScoreRoom<64, 4> | kScoreRoom<64, 8> | kScoreRoom<128, 4> | kScoreRoom<128, 8>) % 16 == 0, "16-byte records");
 template <int GP> constexpr int kRoomBlocks = GP == 4 ? 128 : 64;    // three workgroups fit a CU
 template <int GP> constexpr int kScoreBytes = kRoomBlocks<GP> * 16 * GP * 4;
 // Whether a sequence's rows keep their scores in LDS (weights): its blocks are one
