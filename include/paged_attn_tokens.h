@@ -80,8 +80,8 @@ int paged_attn_extend_tree(const pa_kv_pool *pool, const void *q, const int32_t 
  *     bounds[block][g][0][d] = min K,   bounds[block][g][1][d] = max K,
  * bf16 [num_blocks][num_kv_heads][2][head_dim], beside the pools (so shared
  * blocks share them).  No key of block j can score higher for query head h than
- * sum_d max(q_hd lo_d, q_hd hi_d), that is q_hd hi_d where q_hd >= 0 and q_hd lo_d
- * elsewhere; the sum of that over the heads of a KV head is the block's score, and
+ * sum_d max(q_hd lo_d, q_hd hi_d), that is q_hd hi_d where q_hd > 0, q_hd lo_d where
+ * q_hd < 0 and 0 where q_hd = 0; the sum of that over the heads of a KV head is the block's score, and
  * each (sequence, KV head) attends to
  *     its first_blocks first and last_blocks last blocks, and the blocks of the
  *     highest scores among the others, max_blocks in all

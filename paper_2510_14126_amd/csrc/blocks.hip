@@ -183,34 +183,44 @@ __device__ __forceinline__ void score_blocks(const BlocksParams& p, int b, int g
     }
   }
 
-  auto score = [&](const u32x4_t (&y)[kLoads], int at) {
+  auto score = [&](u32x4_t (&y)[kLoads], int at) {
     double v[kLoads];
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const uint32_t w[4] = {y[i][0], y[i][1], y[i][2], y[i][3]};
-      v[i] = 0.0;
-#pragma unroll
-      for (int d = 0; d < 8; ++d) v[i] = fma(q[d], (double)(d & 1 ? bf16_hi(w[d / 2]) : bf16_lo(w[d / 2])), v[i]);
-    }
-    // lane bits from the block's highest on choose which half stays
     int i;
-    if constexpr (kLanes == 32) {
+    for (bool again = false;; again = true) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = folded<16>(v[k], v[k + 4], lane);
+      for (int k = 0; k < kLoads; ++k) {
+        const uint32_t w[4] = {y[k][0], y[k][1], y[k][2], y[k][3]};
+        v[k] = 0.0;
 #pragma unroll
-      for (int k = 0; k < 2; ++k) v[k] = folded<8>(v[k], v[k + 2], lane);
-      v[0] = folded<4>(v[0], v[1], lane);
-      v[0] += moved<kDppQuadXor2>(v[0]);
-      i = ((lane & 16) >> 2) | ((lane & 8) >> 2) | ((lane & 4) >> 2);
-    } else {
+        for (int d = 0; d < 8; ++d) v[k] = fma(q[d], (double)(d & 1 ? bf16_hi(w[d / 2]) : bf16_lo(w[d / 2])), v[k]);
+      }
+      // lane bits from the block's highest on choose which half stays
+      if constexpr (kLanes == 32) {
 #pragma unroll
-      for (int k = 0; k < 4; ++k) v[k] = folded<8>(v[k], v[k + 4], lane);
+        for (int k = 0; k < 4; ++k) v[k] = folded<16>(v[k], v[k + 4], lane);
 #pragma unroll
-      for (int k = 0; k < 2; ++k) v[k] = folded<4>(v[k], v[k + 2], lane);
-      v[0] = folded<2>(v[0], v[1], lane);
-      i = ((lane & 8) >> 1) | ((lane & 4) >> 1) | ((lane & 2) >> 1);
+        for (int k = 0; k < 2; ++k) v[k] = folded<8>(v[k], v[k + 2], lane);
+        v[0] = folded<4>(v[0], v[1], lane);
+        v[0] += moved<kDppQuadXor2>(v[0]);
+        i = ((lane & 16) >> 2) | ((lane & 8) >> 2) | ((lane & 4) >> 2);
+      } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = folded<8>(v[k], v[k + 4], lane);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) v[k] = folded<4>(v[k], v[k + 2], lane);
+        v[0] = folded<2>(v[0], v[1], lane);
+        i = ((lane & 8) >> 1) | ((lane & 4) >> 1) | ((lane & 2) >> 1);
+      }
+      v[0] += moved<kDppQuadXor1>(v[0]);
+      // A bound that no head's q looks at (no positive part over the greatest, no negative
+      // one over the least) may be infinite, and 0 times it is NaN: once more without those.
+      if (again || __builtin_amdgcn_ballot_w64(v[0] != v[0]) == 0) break;
+#pragma unroll
+      for (int d = 0; d < 8; ++d)
+        if (q[d] == 0.0)
+#pragma unroll
+          for (int k = 0; k < kLoads; ++k) y[k][d / 2] &= d & 1 ? 0x0000ffffu : 0xffff0000u;
     }
-    v[0] += moved<kDppQuadXor1>(v[0]);
     const int block = at + i * kGroups<D> + part;
     if (block < end && lane % (kLanes / kLoads) == 0) store(block, choose::key_of(v[0]));
   };

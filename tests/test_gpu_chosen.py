@@ -274,6 +274,40 @@ def test_choice_of_infinite_and_nan_scores():
     assert t["picked"].cpu().numpy()[0, 0].tolist() == [1, 3, 7, 19]
 
 
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("heads", [1, 3, 8])
+def test_choice_past_bounds_that_no_head_looks_at(heads, d):
+    """q > 0 looks at the greatest values, q < 0 at the least, q = 0 at none: infinities elsewhere do not count."""
+    print(f"[gpu case] infinite bounds on the other side {heads} {d}", flush=True)
+    n = 150
+    c = Sparse(21, ctx=[16 * n], hq=heads, hkv=1, d=d, first=0, last=1, most=41)
+    rng = np.random.default_rng(heads + d)
+    sign = rng.integers(-1, 2, d)                                               # of all heads, so that a side is unused
+    q = sign * rng.integers(1, 9, (heads, d)).astype(np.float64)
+    q[0, :3] = [2, -2, 0]
+    q[1:, :3] = rng.integers(0, 3, (heads - 1, 3)) * np.array([1, -1, 0])
+    c.q[0] = (q.astype(np.float32).view(np.uint32) >> 16).astype(np.uint16)
+    lo = rng.integers(-99, 0, (n, d)).astype(np.float64)
+    hi = rng.integers(0, 99, (n, d)).astype(np.float64)
+    for j in rng.permutation(n)[:90]:                                           # sides that are not looked at
+        lo[j, 0], hi[j, 1] = -np.inf, np.inf
+        lo[j, 2], hi[j, 2] = rng.choice([-np.inf, -1.0]), np.inf
+    lo[5, 3:], hi[5, 3:] = -np.inf, np.inf                                      # looked at: the highest
+    lo[6], hi[6] = np.inf, -np.inf                                              # no number in any dimension: the lowest
+    t = c.setup()
+    c.bound()
+    x = torch.tensor(np.stack([lo, hi], 1)[:, None], device=DEV).to(torch.bfloat16).view(torch.int16)
+    for j in range(n):
+        t["bounds"][int(c.table[0, j])] = x[j]
+    c.select()
+    torch.cuda.synchronize()
+    with np.errstate(all="ignore"):
+        part = np.where(q > 0, q * hi[:, None], np.where(q < 0, q * lo[:, None], 0.0))
+    scores = part.sum((1, 2))
+    assert not np.isnan(scores).any() and scores[5] == np.inf and scores[6] == -np.inf
+    assert t["picked"].cpu().numpy()[0, 0].tolist() == oracle.select_blocks(scores, 0, 1, 41)
+
+
 @pytest.mark.parametrize("hq,hkv,d", [(8, 2, 128), (32, 4, 64), (71, 1, 64), (3, 3, 128)])
 def test_lists_of_the_callers_own(hq, hkv, d):
     """Any order, entries that name no block, blocks listed twice, lists of none."""
