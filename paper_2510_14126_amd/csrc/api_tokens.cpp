@@ -176,8 +176,9 @@ int select_bytes(const pa_kv_pool* pool, int32_t batch, int32_t max_context_len,
   const int rc = check_batch(pool, batch, max_context_len, fn);
   if (rc) return rc;
   if (max_blocks < 1) return fail(PA_EINVAL, "%s: max_blocks = %d < 1", fn, max_blocks);
-  const int64_t blocks = blocks_of(max_context_len);
-  *bytes = blocks > max_blocks ? (size_t)batch * pool->num_kv_heads * blocks * sizeof(uint64_t) : 0;
+  const int64_t blocks = blocks_of(max_context_len), rows = (int64_t)batch * pool->num_kv_heads;
+  if (blocks > max_blocks && rows > kMostBytes / 8 / blocks) return fail(PA_EINVAL, "%s: grid too large", fn);
+  *bytes = blocks > max_blocks ? (size_t)rows * blocks * sizeof(uint64_t) : 0;
   return PA_OK;
 }
 

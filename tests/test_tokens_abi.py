@@ -155,6 +155,9 @@ def test_workspace_sizes():
                     (pa.paged_attn_tree_workspace_size, (1, 8, 1000, 300))):
         with pytest.raises(pa.PagedAttnError):
             fn(pool, *bad)
+    many = pa.kv_pool_create(8, 16, 64, 64, A, A)                                # 2^66 bytes: no size_t holds them
+    with pytest.raises(pa.PagedAttnError):
+        pa.paged_attn_select_workspace_size(many, BIG, 2 ** 30 - 1, 5)
 
 
 # --------------------------------------------------------------------------
