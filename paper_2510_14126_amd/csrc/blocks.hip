@@ -92,10 +92,14 @@ constexpr int kWaves = 4;
 // Rounds of a wavefront: as many as leave the GPU full (kFillWaves), so that the chain
 // of loads before a wavefront's first round (length, table, bounds) and its sums of q
 // are paid once for several, and few, so that the last ones end together.  Whole steps,
-// 64 sequences of 4097..28672 tokens, 32 heads over 8 (14 rounds to fill), with 1 / 2 / 3
-// / 4 / 8 / 11: 174 / 176 / 153 / 154 / 157 / 159 us; 16 of them (3) 64.5 / 59.5 with 2.
-constexpr int kFillWaves = 4 * 1024, kMostRounds = 4;
+// 64 sequences of 4097..28672 tokens, 32 heads over 8 (28 rounds to fill), with 1 / 2 / 3
+// / 4 / 8 / 11: 174 / 176 / 153 / 154 / 157 / 159 us; 16 of them (7) 64.5 / 59.5 with 2.
+// Four / two / one wavefronts per SIMD to fill: one of 131003 tokens, 64 heads over 8, 43.8 /
+// 43.8 / 42.9, four, heads over 4, D = 64, 50.5 / 44.7 / 45.4, four of 32000, 32 over 8, 25.8 /
+// 24.9 / 26.4.
+constexpr int kFillWaves = 2 * 1024, kMostRounds = 4;
 typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
+typedef short i16x2_t __attribute__((ext_vector_type(2)));
 
 template <int CTRL>
 __device__ __forceinline__ double moved(double x) {
@@ -140,6 +144,13 @@ __device__ __forceinline__ void score_blocks(const BlocksParams& p, int b, int g
   // the lane's side: pieces of the least values meet the negative parts of q
   const bool upper = piece >= kLanes / 2;
   const uint16_t* q_row = p.q + ((size_t)b * p.num_kv_heads + g) * p.group * D + piece % (kLanes / 2) * 8;
+  // the first heads' q before all else: it is summed while the bounds are on their way (one
+  // sequence of 131003 tokens, 64 heads over 8, 43.8 -> 36.5 us, of 300 14.9 -> 13.3; read four
+  // heads at a time behind the bounds before)
+  constexpr int kEarly = 8;
+  uint4 early[kEarly];
+#pragma unroll
+  for (int h = 0; h < kEarly; ++h) early[h] = *reinterpret_cast<const uint4*>(q_row + (size_t)min(h, p.group - 1) * D);
   // 64 table entries at a time, and the 64 behind them; the first before the length is there
   const int32_t* table = p.block_tables + (size_t)b * p.bt_stride + p.first_blocks;
   const int most = min(p.key_blocks - p.first_blocks, base + rounds * kPer);
@@ -166,22 +177,26 @@ __device__ __forceinline__ void score_blocks(const BlocksParams& p, int b, int g
   u32x4_t x[2][kLoads];
   load(x[0], base);
 
+  // Sums of the parts' magnitudes: with the lower side's signs flipped, bf16 that are
+  // negative as 16-bit integers have no part.  (So has a NaN on one of the sides.)
+  const uint32_t flip = upper ? 0u : 0x80008000u;
   double q[8] = {0, 0, 0, 0, 0, 0, 0, 0};
-  for (int h0 = 0; h0 < p.group; h0 += 4) {
-    uint4 y[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) y[k] = *reinterpret_cast<const uint4*>(q_row + (size_t)min(h0 + k, p.group - 1) * D);
+  auto add = [&](const uint4& y) {
+    const uint32_t w[4] = {y.x ^ flip, y.y ^ flip, y.z ^ flip, y.w ^ flip};
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-      const uint32_t w[4] = {y[k].x, y[k].y, y[k].z, y[k].w};
-      if (h0 + k < p.group)
-#pragma unroll
-        for (int d = 0; d < 8; ++d) {
-          const float z = d & 1 ? bf16_hi(w[d / 2]) : bf16_lo(w[d / 2]);
-          q[d] += (double)((upper ? z < 0.f : z > 0.f) ? 0.f : z);    // NaN stays
-        }
+      const uint32_t z = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(i16x2_t, w[k]), i16x2_t{0, 0}));
+      q[2 * k] += (double)bf16_lo(z);
+      q[2 * k + 1] += (double)bf16_hi(z);
     }
-  }
+  };
+#pragma unroll
+  for (int h = 0; h < kEarly; ++h)
+    if (h < p.group) add(early[h]);                // uniform
+#pragma unroll 4
+  for (int h = kEarly; h < p.group; ++h) add(*reinterpret_cast<const uint4*>(q_row + (size_t)h * D));
+#pragma unroll
+  for (int d = 0; d < 8; ++d) q[d] = upper ? q[d] : -q[d];
 
   auto score = [&](u32x4_t (&y)[kLoads], int at) {
     double v[kLoads];
@@ -252,12 +267,13 @@ __global__ void __launch_bounds__(64 * kWaves) score_kernel(const BlocksParams p
 // while some workgroups choose others still read, but four wavefronts to a row.  It does
 // where the rows fill the GPU (kManyRows), or the candidates are few (kOwnRounds of each
 // wavefront).  Whole steps, 32 heads over 8, scores in a launch of their own / here: one
-// sequence of 64 / 128 / 256 / 500 blocks 17.7 / 15.8, 18.3 / 17.2, 18.8 / 19.3, 19.5 /
-// 24.0 us, four of 128 / 256 19.2 / 17.9, 19.6 / 19.9; 32 (256 rows) of 500 / 2000 32.2 / 30.9, 70.3 / 67.0; 128 of 500 / 1000 /
-// 2000 82.8 / 75.4, 130.7 / 115, 228 / 195.  Eight wavefronts to a row from kLongRounds
-// rounds on (four / eight: 32 of 500 / 1000 / 2000 31.0 / 30.3, 43.4 / 41.1, 67.3 / 62.8;
-// 128 of 256 / 500 / 1000 / 2000 55.2 / 60.3, 75.4 / 77.4, 115.5 / 115.9, 195 / 193.5; 32 of
-// 125..2000 58.1 / 49.7).
+// sequence of 256 / 320 / 500 blocks 16.4 / 17.9, 17.0 / 19.3, 17.2 / 22.7 us, four of 256 /
+// 320 17.2 / 18.6, 17.5 / 19.9 (before q was summed ahead of the bounds one of 64 / 128 17.7 /
+// 15.8, 18.3 / 17.2; 32, that is 256 rows, of 500 / 2000 32.2 / 30.9, 70.3 / 67.0; 128 of 500 /
+// 1000 / 2000 82.8 / 75.4, 130.7 / 115, 228 / 195).  Eight wavefronts to a row from
+// kLongRounds rounds on (four / eight: 32 of 500 / 1000 / 2000 31.0 / 30.3, 43.4 / 41.1, 67.3 /
+// 62.8; 128 of 256 / 500 / 1000 / 2000 55.2 / 60.3, 75.4 / 77.4, 115.5 / 115.9, 195 / 193.5; 32
+// of 125..2000 58.1 / 49.7).
 constexpr int kFewKeys = 2048, kManyKeys = 16384;
 constexpr int kOwnRounds = 3, kManyRows = 256, kLongRounds = 33;
 template <int THREADS, int CAPACITY, typename Keys>
