@@ -250,6 +250,30 @@ def test_choice_of_close_and_equal_scores(d):
     assert np.array_equal(t["picked"].cpu().numpy()[0, 0], list(range(39)) + [n - 1])
 
 
+@pytest.mark.parametrize("n,coarse,fine", [(1500, 30, 3), (1500, 64, 1), (1500, 65, 5), (5000, 60, 64), (5000, 50, 100), (1030, 1, 1)])
+def test_choice_by_bits_far_below_the_first_that_differ(n, coarse, fine):
+    """Groups of scores that only bits 2^-32 of the largest tell apart, and within them groups of equal ones."""
+    print(f"[gpu case] low bits {n} {coarse} {fine}", flush=True)
+    c = Sparse(9, ctx=[16 * n], hq=1, hkv=1, d=64, first=0, last=1, most=n // 3)
+    rng = np.random.default_rng(n)
+    c.k[:] = 0
+    c.q[:] = 0
+    c.q[0, 0, 0], c.q[0, 0, 5], c.q[0, 0, 63] = 0x4580, 0x4580, 0x3B80           # 4096, 4096, 2^-8
+    order = rng.permutation(n)
+    scores = np.zeros(n)
+    for j in range(2, n):                                                        # the first two: 0
+        block, hi, lo = c.table[0, j], order[j] // coarse % 200, order[j] % coarse // fine
+        c.k[block, :, 2, 0] = 0x4580
+        c.k[block, :, 7, 5] = bits_of(float(hi))
+        c.k[block, :, 5, 63] = bits_of(float(lo))
+        scores[j] = 2.0 ** 24 + 4096.0 * hi + lo / 256
+    t = c.setup()
+    c.bound()
+    c.select()
+    torch.cuda.synchronize()
+    assert t["picked"].cpu().numpy()[0, 0].tolist() == oracle.select_blocks(scores, 0, 1, n // 3)
+
+
 def bits_of(x):
     return int(np.float32(x).view(np.uint32) >> 16)
 
@@ -272,6 +296,23 @@ def test_choice_of_infinite_and_nan_scores():
     c.select()
     torch.cuda.synchronize()
     assert t["picked"].cpu().numpy()[0, 0].tolist() == [1, 3, 7, 19]
+
+
+@pytest.mark.parametrize("nan", [0x7FC0, 0xFFC0])
+def test_choice_of_a_query_that_is_nan(nan):
+    """All scores of its KV head are NaN, the highest: the lowest blocks.  The others choose as ever."""
+    print(f"[gpu case] nan in q {nan:x}", flush=True)
+    c = Sparse(22, ctx=[900, 2000], hq=22, hkv=2, d=128, first=1, last=2, most=30)
+    want = c.oracle_picks()
+    c.q[1, 15, 77] = nan                                                        # the fifth of eleven heads
+    c.q[0, 10, 0] = nan                                                         # the last
+    c.setup()
+    c.bound()
+    c.select()
+    torch.cuda.synchronize()
+    for b, g, n in ((1, 1, 125), (0, 0, 57)):
+        want[b, g] = list(range(28)) + [n - 2, n - 1]
+    assert np.array_equal(c.t["picked"].cpu().numpy(), want)
 
 
 @pytest.mark.parametrize("d", [64, 128])

@@ -58,6 +58,29 @@ def test_choice(kind, keep, recent):
             assert lens[b] == len(want) and kept[b, :len(want)].tolist() == want and (kept[b, len(want):] == -1).all()
 
 
+@pytest.mark.parametrize("equal", [1, 2, 63, 64, 65, 300])
+@pytest.mark.parametrize("n", [1025, 1100, 2048, 2049, 9000, 32768, 32769])
+def test_equal_totals_on_the_threshold(n, equal):
+    """Groups of equal totals that the cut goes through, as many as a wavefront's lanes and more, among others close by."""
+    print(f"[gpu case] keep on the threshold {n} {equal}", flush=True)
+    rng = np.random.default_rng(n + equal)
+    above = 400
+    totals = np.zeros((4, n), np.float32)
+    cuts = [1, equal // 2, equal, equal + 1]
+    for b in range(4):
+        x = (np.uint32(0x3F000000) - rng.integers(1, 1 << 20, n).astype(np.uint32)).view(np.float32)    # below 0.5
+        at = rng.permutation(n)
+        x[at[:above]] = 0.5 + rng.random(above, np.float32) + np.float32(0.001)
+        x[at[above:above + equal]] = 0.5
+        if b == 1:
+            x[at[-1]] = -1e30                              # the first bit that differs is the sign
+        totals[b] = x
+    for cut in cuts:
+        kept, lens = choose(totals, [n] * 4, None, 0, above + cut)
+        for b in range(4):
+            assert kept[b, :lens[b]].tolist() == oracle.keep_heaviest(totals[b], 0, 0, above + cut)
+
+
 def test_choice_of_long_sequences():
     print("[gpu case] keep long", flush=True)
     rng = np.random.default_rng(3)
