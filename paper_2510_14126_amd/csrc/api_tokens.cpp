@@ -66,11 +66,18 @@ int launched(hipError_t e, const char* fn) {
 
 // How the rows of a decode and their blocks are dealt to workgroups: tiles of four or
 // eight heads of a KV head, and partitions of a row's blocks as in the biased decode.
+//
+// Where the rows fill the GPU, those with kept weights are split at kMostBlocks (whose
+// scores LDS holds), but into pieces of kLongBlocks: a workgroup takes a hundred
+// microseconds for 128 blocks, and the last ones' end is what the others wait for.  Split
+// at 128 into 128 / at 128 into 64 / at 64 into 64 / at 128 into 32: 128 sequences of 64..8192
+// tokens 169 / 160 / 167 / 162 us, 64 of 64..16000 92 / 85 / 88 / 86; 128 of an equal
+// distribution of 64..8192 438 / 432 / 435 / 440, 64 of 4096 201 / 203 / 203 / 207.
 constexpr int64_t kFill128 = 256, kFill64 = 512;
-constexpr int64_t kWholeBlocks = 40, kLeastBlocks = 16, kMostBlocks = 128;
+constexpr int64_t kWholeBlocks = 40, kLeastBlocks = 16, kMostBlocks = 128, kLongBlocks = 64;
 
 struct Plan {
-  int32_t tile_heads, head_tiles, parts, part_blocks;
+  int32_t tile_heads, head_tiles, parts, part_blocks, whole_blocks;
   int64_t tiles;                          // row tiles: batch x head tiles x KV heads
   size_t o_bytes, lse_bytes, score_bytes;
   size_t bytes() const { return o_bytes + lse_bytes + score_bytes; }
@@ -91,6 +98,8 @@ int plan_decode(const pa_kv_pool* pool, int32_t batch, int32_t num_q_heads, int6
     const int64_t parts = std::max<int64_t>(1, (pool->head_dim == 64 ? kFill64 : kFill128) / std::max<int64_t>(pl->tiles, 1));
     per = std::min(kMostBlocks, std::max(kLeastBlocks, (blocks + 2 * parts - 1) / (2 * parts) * 2));
   }
+  pl->whole_blocks = (int32_t)per;
+  if (weights && per == kMostBlocks && blocks > kMostBlocks) per = kLongBlocks;
   const int64_t parts = std::max<int64_t>(1, (blocks + per - 1) / per);
   pl->part_blocks = (int32_t)per;
   pl->parts = (int32_t)parts;
@@ -137,6 +146,7 @@ int decode_params(const pa_kv_pool* pool, const void* q, const int32_t* block_ta
   p->max_ctx = max_context_len;
   p->parts = pl.parts;
   p->part_blocks = pl.part_blocks;
+  p->whole_blocks = pl.whole_blocks;
   p->stream_tiles = pl.head_tiles == 1 && pool->shared_blocks == 0;
   p->scale_log2 = (float)(scale * kLog2e);
   return PA_OK;

@@ -17,7 +17,7 @@
 // These stores cost more than their bytes (128 sequences of 64..8192 tokens, 32 heads
 // over 8, 782 MB of K and V and 24 MB of scores: 172 us, 150 without the stores), so they
 // are kept down.  A wavefront gathers scores in LDS, up to kRoomBlocks a workgroup; a
-// row whose blocks are one partition of no more than that ends with its log-sum-exps at
+// row whose blocks are no more than that is one partition, and ends with its log-sum-exps at
 // hand, and what goes to memory is one sum over the tile's heads a token, a fourth or an
 // eighth (164 us; 128 of 64..2000 118 / 106).  The others' scores are stored 64 blocks at a time.
 #pragma once
@@ -64,10 +64,10 @@ static_assert((kScoreRoom<64, 4> | kScoreRoom<64, 8> | kScoreRoom<128, 4> | kSco
 template <int GP> constexpr int kRoomBlocks = GP == 4 ? 128 : 64;    // three workgroups fit a CU
 template <int GP> constexpr int kScoreBytes = kRoomBlocks<GP> * 16 * GP * 4;
 // Whether a sequence's rows keep their scores in LDS (weights): its blocks are one
-// partition, and there is room.
+// partition then.
 template <int GP>
 __device__ __forceinline__ bool kept_whole(const TokensParams& p, int nblk) {
-  return nblk <= kRoomBlocks<GP> && nblk <= p.part_blocks;
+  return nblk <= min(p.whole_blocks, kRoomBlocks<GP>);
 }
 template <int D, int GP> constexpr int kLsePlace = 2 * kWaves * GP + kWaves * GP * D;         // floats: behind the merge's
 template <int D, int GP, bool WEIGHTS>
@@ -106,7 +106,8 @@ __device__ __forceinline__ void decode_body(const TokensParams& p, int wg, lds_u
   const int ctx = clamped(p.context_lens[at.b], p.max_ctx);
   const int nblk = (ctx + 15) >> 4;
   const int all = LISTED ? (ctx > 0 ? p.max_blocks : 0) : nblk;
-  const int cnt = min(p.part_blocks, all - j0);
+  const bool whole = WEIGHTS && kept_whole<GP>(p, nblk);
+  const int cnt = whole ? (at.part == 0 ? nblk : 0) : min(p.part_blocks, all - j0);
   const int tile_index = (at.b * p.head_tiles + at.tile) * p.num_kv_heads + at.g;
   const size_t slot = (size_t)tile_index * p.parts + at.part;
   if (cnt <= 0 && at.part > 0) {
@@ -114,7 +115,6 @@ __device__ __forceinline__ void decode_body(const TokensParams& p, int wg, lds_u
     return;
   }
   float* scores = WEIGHTS ? p.scores + (size_t)tile_index * p.score_tokens * GP : nullptr;
-  const bool whole = WEIGHTS && kept_whole<GP>(p, nblk);
   lds_f32_t* room = reinterpret_cast<lds_f32_t*>(smem + kScoreRoom<D, GP> + wave * (kScoreBytes<GP> / kWaves));
 
   WaveState<D> S;

@@ -39,6 +39,7 @@ struct TokensParams {
   int32_t score_tokens;          // max_ctx rounded up to whole blocks
   int32_t parts;                 // partitions of a row's blocks
   int32_t part_blocks;           // blocks of one
+  int32_t whole_blocks;          // weights: rows of no more are one partition, if LDS holds their scores
   int32_t stream_tiles;          // 1: load the tiles with the streaming cache hint
   float scale_log2;              // scale * log2(e)
 };

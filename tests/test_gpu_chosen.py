@@ -397,6 +397,10 @@ WEIGHTS = {
     "one_long_64": dict(ctx=[33333], hq=4, hkv=1, d=64),
     "zero_scale": dict(ctx=[200, 17], hq=8, hkv=2, d=128, scale=0.0),
     "negative_scale": dict(ctx=[200, 17], hq=8, hkv=2, d=128, scale=-0.1),
+    # rows that fill the GPU: some kept whole, some split
+    "filled": dict(ctx=[2048, 2049, 1024, 1025, 2500, 0, 1, 2047, 2064, 4000] + [9, 40, 70] * 10, hq=32, hkv=8, d=128),
+    "filled_eights": dict(ctx=[1024, 1025, 2048, 2049, 3000, 0, 513] + [3, 31, 65] * 11, hq=48, hkv=8, d=128),
+    "filled_64": dict(ctx=[2048, 2049, 1025, 2100, 0, 1008] + [2, 16, 90] * 20, hq=8, hkv=8, d=64),
 }
 
 
