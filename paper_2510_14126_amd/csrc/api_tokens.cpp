@@ -65,7 +65,11 @@ int launched(hipError_t e, const char* fn) {
 }
 
 // How the rows of a decode and their blocks are dealt to workgroups: tiles of four or
-// eight heads of a KV head, and partitions of a row's blocks as in the biased decode.
+// eight heads of a KV head, and partitions of a row's blocks as in the biased decode:
+// as many as make a workgroup a CU (kFill64: two), or twice that rather than partitions of
+// more than kMostBlocks.  Capped at kMostBlocks / twice as many, 32 heads over 8: weights of
+// four sequences of 15000..30000 tokens 81 / 74.5 us, of one of 130000, 64 heads, 120 / 113;
+// 1500 chosen blocks of four 100 / 96; three of 64..30000 43 / 45.
 //
 // Where the rows fill the GPU, those with kept weights are split at kMostBlocks (whose
 // scores LDS holds), but into pieces of kLongBlocks: a workgroup takes a hundred
@@ -95,11 +99,16 @@ int plan_decode(const pa_kv_pool* pool, int32_t batch, int32_t num_q_heads, int6
   if (pl->tiles > 0x7fffffffLL) return fail(PA_EINVAL, "%s: grid too large", fn);
   int64_t per = std::max<int64_t>(blocks, 1);
   if (blocks > kWholeBlocks) {
-    const int64_t parts = std::max<int64_t>(1, (pool->head_dim == 64 ? kFill64 : kFill128) / std::max<int64_t>(pl->tiles, 1));
-    per = std::min(kMostBlocks, std::max(kLeastBlocks, (blocks + 2 * parts - 1) / (2 * parts) * 2));
+    const int64_t fill = pool->head_dim == 64 ? kFill64 : kFill128;
+    auto deal = [&](int64_t workgroups) {
+      const int64_t parts = std::max<int64_t>(1, workgroups / std::max<int64_t>(pl->tiles, 1));
+      per = std::max(kLeastBlocks, (blocks + 2 * parts - 1) / (2 * parts) * 2);
+    };
+    deal(fill);
+    if (per > kMostBlocks) deal(2 * fill);
   }
-  pl->whole_blocks = (int32_t)per;
-  if (weights && per == kMostBlocks && blocks > kMostBlocks) per = kLongBlocks;
+  pl->whole_blocks = (int32_t)std::min(per, kMostBlocks);
+  if (per > kMostBlocks) per = weights ? kLongBlocks : kMostBlocks;
   const int64_t parts = std::max<int64_t>(1, (blocks + per - 1) / per);
   pl->part_blocks = (int32_t)per;
   pl->parts = (int32_t)parts;

@@ -109,6 +109,7 @@ SPARSE = {
     "many": dict(ctx=[20 + 41 * i for i in range(60)], hq=8, hkv=2, d=128, first=1, last=1, most=17),
     "long": dict(ctx=[30000, 9001], hq=8, hkv=2, d=64, first=1, last=4, most=150),
     "very_long": dict(ctx=[70001], hq=4, hkv=1, d=64, first=4, last=16, most=256),
+    "long_lists": dict(ctx=[6500, 5000] + [300, 17, 0] * 5, hq=8, hkv=8, d=128, first=1, last=1, most=390),
     "negative_scale": dict(ctx=[700], hq=8, hkv=2, d=128, first=0, last=1, most=9, scale=-0.1),
     "many_rows": dict(ctx=[30 + 61 * i for i in range(65)], hq=8, hkv=4, d=64, first=0, last=1, most=10),
     "many_long_rows": dict(ctx=[5 + 141 * i for i in range(65)], hq=8, hkv=4, d=128, first=1, last=1, most=30),
@@ -397,6 +398,7 @@ WEIGHTS = {
     "one_long_64": dict(ctx=[33333], hq=4, hkv=1, d=64),
     "zero_scale": dict(ctx=[200, 17], hq=8, hkv=2, d=128, scale=0.0),
     "negative_scale": dict(ctx=[200, 17], hq=8, hkv=2, d=128, scale=-0.1),
+    "two_a_cu": dict(ctx=[6000, 4097, 2500] + [20, 1030, 700, 1] * 3 + [0], hq=8, hkv=8, d=128),
     # rows that fill the GPU: some kept whole, some split
     "filled": dict(ctx=[2048, 2049, 1024, 1025, 2500, 0, 1, 2047, 2064, 4000] + [9, 40, 70] * 10, hq=32, hkv=8, d=128),
     "filled_eights": dict(ctx=[1024, 1025, 2048, 2049, 3000, 0, 513] + [3, 31, 65] * 11, hq=48, hkv=8, d=128),
