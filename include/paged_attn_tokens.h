@@ -214,8 +214,10 @@ int paged_attn_keep_heaviest(const float *totals, int64_t totals_stride,
  *                    be: blocks that hold no token which this call reads, but for
  *                    the one in which first_tokens[b] lies, which may be the same;
  *                    or NULL (dst_stride 0): block_tables, in place
- *   first_tokens     device int32 [batch], or NULL: 0.  Tokens before it stay
- *   context_lens     device int32 [batch], before the move (read for totals alone)
+ *   first_tokens     device int32 [batch], or NULL: 0.  Tokens before it stay.  A
+ *                    sequence of fewer tokens (a padded slot of none) keeps what it
+ *                    has and nothing of it moves
+ *   context_lens     device int32 [batch], before the move
  *   kept             device int32 [batch][kept_stride], each row ascending without
  *                    equal ones (else what the moved tokens hold is unspecified)
  *   kept_lens        device int32 [batch]
@@ -223,8 +225,9 @@ int paged_attn_keep_heaviest(const float *totals, int64_t totals_stride,
  *                    both NULL: moved with the tokens; the first ones' are copied and
  *                    those of the tokens behind the moved ones, up to n_b, become 0.
  *                    The same pointer (in place), or not overlapping
- *   new_lens         device int32 [batch], or NULL: first_tokens[b] + kept_lens[b];
- *                    may be context_lens
+ *   new_lens         device int32 [batch], or NULL: first_tokens[b] + kept_lens[b], or
+ *                    context_lens[b] where that is below first_tokens[b]; may be
+ *                    context_lens
  * A block that a row of dst_tables (or block_tables, in place) writes belongs to
  * that sequence alone.  dst_stride need not reach max_context_len: tokens whose place
  * is beyond that table are not moved. */

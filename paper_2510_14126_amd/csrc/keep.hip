@@ -56,6 +56,23 @@ __device__ __forceinline__ void all_loaded() {
   __syncthreads();
 }
 
+// What a sequence keeps: its first tokens, and how many of its list move behind them.  A
+// sequence that is shorter than its first tokens keeps what it has, and nothing moves: it must
+// not grow to tokens that it never held.
+//
+// new_lens may be context_lens, so another workgroup may have written first + moved there
+// already: that gives the same two numbers again (first <= context: first is below the sum,
+// and moved does not depend on the context; else the sum is the context and moved 0).
+struct Stay {
+  int first, moved;
+};
+__device__ __forceinline__ Stay stay_of(const CompactParams& p, int b) {
+  const int ctx = clamped(p.context_lens[b], p.max_ctx);
+  const int first = p.first_tokens ? clamped(p.first_tokens[b], p.max_ctx) : 0;
+  const int most = min(p.kept_stride, p.max_ctx - first);
+  return {min(first, ctx), first <= ctx ? clamped(p.kept_lens[b], most) : 0};
+}
+
 // AHEAD: the first round's entries of the list are loaded before its length is there.
 // That is a link less in the chain of loads (lengths, list, table, rows), which is the
 // time of a small move, and registers, which large ones miss: four sequences cut to 256
@@ -80,8 +97,7 @@ __device__ __forceinline__ void move_rows(const CompactParams& p, int wg) {
 #pragma unroll
     for (int i = 0; i < kPasses; ++i) early[i] = own0 + i * kRows + row < p.kept_stride ? kept[own0 + i * kRows + row] : 0;
   }
-  const int first = p.first_tokens ? clamped(p.first_tokens[b], p.max_ctx) : 0;
-  const int m = clamped(p.kept_lens[b], min(p.kept_stride, p.max_ctx - first));
+  const auto [first, m] = stay_of(p, b);
   const int32_t* from = p.block_tables + (size_t)b * p.bt_stride;
   const int32_t* to = p.dst_tables ? p.dst_tables + (size_t)b * p.dst_stride : from;
   const int to_blocks = p.dst_tables ? p.dst_stride : p.bt_stride;
@@ -115,8 +131,7 @@ __device__ __forceinline__ void move_rows(const CompactParams& p, int wg) {
 
 // A sequence's totals, in the same way, and its new length.
 __device__ __forceinline__ void move_totals(const CompactParams& p, int b) {
-  const int first = p.first_tokens ? clamped(p.first_tokens[b], p.max_ctx) : 0;
-  const int m = clamped(p.kept_lens[b], min(p.kept_stride, p.max_ctx - first));
+  const auto [first, m] = stay_of(p, b);
   const int ctx = clamped(p.context_lens[b], p.max_ctx);
   if (p.totals_out) {
     const int32_t* kept = p.kept + (size_t)b * p.kept_stride;
