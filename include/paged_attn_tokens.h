@@ -227,7 +227,7 @@ int paged_attn_keep_heaviest(const float *totals, int64_t totals_stride,
  *                    The same pointer (in place), or not overlapping
  *   new_lens         device int32 [batch], or NULL: first_tokens[b] + kept_lens[b], or
  *                    context_lens[b] where that is below first_tokens[b]; may be
- *                    context_lens
+ *                    context_lens, and no other array of the call (PA_EINVAL)
  * A block that a row of dst_tables (or block_tables, in place) writes belongs to
  * that sequence alone.  dst_stride need not reach max_context_len: tokens whose place
  * is beyond that table are not moved. */

@@ -432,6 +432,10 @@ int paged_attn_compact(const pa_kv_pool* pool, const int32_t* block_tables, int3
   if (!aligned(block_tables, 4) || !aligned(dst_tables, 4) || !aligned(first_tokens, 4) || !aligned(context_lens, 4) ||
       !aligned(kept, 4) || !aligned(kept_lens, 4) || !aligned(new_lens, 4))
     return fail(PA_EINVAL, "%s: an index or length array is not 4-byte aligned", fn);
+  // one workgroup of a sequence writes its new length while the others read these
+  if (new_lens && (new_lens == first_tokens || new_lens == kept_lens || new_lens == kept || new_lens == block_tables ||
+                   new_lens == dst_tables))
+    return fail(PA_EINVAL, "%s: new_lens is another of the call's arrays than context_lens", fn);
   pa::CompactParams p{};
   p.k_pool = pool->k;
   p.v_pool = pool->v;
