@@ -213,7 +213,8 @@ int paged_attn_keep_heaviest(const float *totals, int64_t totals_stride,
  *   dst_tables       device int32 [batch][dst_stride], of the tokens as they will
  *                    be: blocks that hold no token which this call reads, but for
  *                    the one in which first_tokens[b] lies, which may be the same;
- *                    or NULL (dst_stride 0): block_tables, in place
+ *                    or NULL (dst_stride 0), or block_tables itself with its
+ *                    bt_stride: in place
  *   first_tokens     device int32 [batch], or NULL: 0.  Tokens before it stay.  A
  *                    sequence of fewer tokens (a padded slot of none) keeps what it
  *                    has and nothing of it moves

@@ -436,6 +436,12 @@ int paged_attn_compact(const pa_kv_pool* pool, const int32_t* block_tables, int3
   if (new_lens && (new_lens == first_tokens || new_lens == kept_lens || new_lens == kept || new_lens == block_tables ||
                    new_lens == dst_tables))
     return fail(PA_EINVAL, "%s: new_lens is another of the call's arrays than context_lens", fn);
+  // the table itself as the second one: several workgroups to a sequence's rows would read
+  // what others of them write
+  if (dst_tables == block_tables && dst_stride == bt_stride) {
+    dst_tables = nullptr;
+    dst_stride = 0;
+  }
   pa::CompactParams p{};
   p.k_pool = pool->k;
   p.v_pool = pool->v;
