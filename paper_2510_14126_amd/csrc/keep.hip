@@ -67,10 +67,10 @@ struct Stay {
   int first, moved;
 };
 __device__ __forceinline__ Stay stay_of(const CompactParams& p, int b) {
-  const int ctx = clamped(p.context_lens[b], p.max_ctx);
-  const int first = p.first_tokens ? clamped(p.first_tokens[b], p.max_ctx) : 0;
-  const int most = min(p.kept_stride, p.max_ctx - first);
-  return {min(first, ctx), first <= ctx ? clamped(p.kept_lens[b], most) : 0};
+  const int lists = p.kept_lens[b], given = p.first_tokens ? p.first_tokens[b] : 0, len = p.context_lens[b];   // together
+  const int ctx = clamped(len, p.max_ctx), first = clamped(given, p.max_ctx);
+  const int moved = clamped(lists, min(p.kept_stride, p.max_ctx - first));
+  return {min(first, ctx), first <= ctx ? moved : 0};
 }
 
 // AHEAD: the first round's entries of the list are loaded before its length is there.
