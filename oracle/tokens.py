@@ -128,7 +128,3 @@ def compact(pool, table, to, first, kept):
         s, d = first + int(t), first + j
         out[to[d // BLOCK], :, d % BLOCK] = pool[table[s // BLOCK], :, s % BLOCK]
     return out
-
-
-def pool_f64(pool):
-    return bf16_to_f64(pool)
