@@ -11,7 +11,8 @@
  *   - the move of chosen tokens to the front of their sequences, which takes
  *     rejected drafts and evicted tokens out of the cache.
  *
- * They are for serving: none has a backward pass, as the library has none.
+ * They are for serving: none has a backward pass, as the library has none.  Calls that may
+ * run at the same time, replays of captured graphs among them, need a workspace each.
  * Device data is clamped as everywhere: lengths into [0, max_context_len], ids
  * into the pool, rows into total_q.
  */

@@ -38,15 +38,19 @@ __global__ void __launch_bounds__(THREADS) keep_kernel(const KeepParams p) {
 // that is enough.  A row moves to a slot at or before its own, and what a later
 // round reads lies behind every slot that this one writes (kept ascends, so row j's
 // source is at least slot j), so only the rows of one round can stand in each
-// other's way.  To other blocks the rounds are workgroups of their own (chunks).
+// other's way.  To other blocks the rounds are workgroups of their own (chunks).  In place
+// they wait for one another: right for an accepted path, slow for a few long lists, whose
+// workgroups are few (8 KV heads of 128, 16384 of 30000 tokens of one sequence 837 us, to
+// other blocks 41; 4096 each of 64 sequences 529 / 450).
 //
 // The rows are read and written once; nothing but their traffic bounds the move.  It
 // reads and writes them with the non-temporal hint, and the KV heads run fastest over
 // the workgroups, then the rounds: neighbouring workgroups then move the rows of
 // the same tokens, 256 bytes of each block's neighbouring tiles.  64 sequences of
 // 3001..15000 tokens cut to 4096, 1.5 GB read and written: rounds fastest 640 us, heads
-// fastest 505, with the hint on loads / stores / both 347 / 343 / 337 (4.6 TB/s, a large
-// copy runs at 4.8); one of 30000 cut to 16384 117 / 93 / 89 / 81 (no hint / ...).
+// fastest 505, with the hint on loads / stores / both 347 / 343 / 337 (4.6 TB/s, a copy of
+// 1 GiB runs at 5.0); one of 30000 cut to 16384, with its choice, 117 / 93 / 89 / 81 (no hint
+// / ...; 66 with the later choice, the move alone 41).
 constexpr int kPasses = kMovePasses;
 typedef unsigned int u32x4_t __attribute__((ext_vector_type(4)));
 
